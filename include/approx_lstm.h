@@ -481,6 +481,125 @@ approx_lstm_status approx_lstm_exact_set_launch(approx_lstm_exact* m, int32_t bl
 approx_lstm_status approx_lstm_exact_set_start_wait(approx_lstm_exact* m, double wait_us);
 void approx_lstm_exact_destroy(approx_lstm_exact* m);
 
+/*
+ * Gated linear recurrence -- the LSTM cell (Sec. II, Fig. 1) whose gates depend
+ * on the input alone, so that time is a scan instead of a chain of matrix
+ * products: from gate pre-activations p_t (rows i, f, g, o; without the bias)
+ *
+ *     c_t = sigmoid(f_t) c_{t-1} + sigmoid(i_t) tanh(g_t),   h_t = sigmoid(o_t) tanh(c_t).
+ *
+ * Stateless calls on the current device.  p, h_out and their gradients hold
+ * `dtype` (0 = fp32, 1 = bf16); the state, the bias and their gradients are
+ * fp32, and so is all arithmetic.  Results do not depend on the device's load:
+ * every sum has a fixed order.
+ *
+ * approx_lstm_linear_run -- the recurrence over a sequence, or (T = 1) one token.
+ *   p        device [T][B][4H]
+ *   bias     device fp32 [4H] or NULL (zeros), added to p
+ *   T, B, H  T >= 0, B >= 1, H >= 1
+ *   lengths  device int32 [B] or NULL (all T): sequence b has timesteps 0 ..
+ *            lengths[b]-1 (values outside [0, T] are taken as the nearer end);
+ *            past them its state stays, h is zero and p is not looked at
+ *   c0       device fp32 [B][H] or NULL (zeros)
+ *   h_out    device [T][B][H], dtype
+ *   c_out    device fp32 [B][H] or NULL: the state after the last timestep; may
+ *            be c0 itself
+ *   c_save   device fp32 [ceil(T / 8)][B][H] or NULL: the state before timesteps
+ *            0, 8, 16, ... (APPROX_LSTM_LINEAR_SAVE), for the backward pass
+ *   workspace, workspace_bytes   device, 16-byte aligned, at least what
+ *            approx_lstm_linear_workspace says for (T, B, H, backward = 0); may be
+ *            NULL where that is 0.  Its contents need not be kept or cleared;
+ *            calls that may overlap (two streams, two captured graphs replayed
+ *            at once) need one each
+ * T = 0 copies c0 to c_out.  Asynchronous on hip_stream, allocates nothing, can
+ * be captured.  p, h_out and c_save must not overlap.
+ *
+ * approx_lstm_linear_backward -- gradients of a scalar from those of h_out and
+ * c_out, on the inputs of the run and the c_save that it wrote.
+ *   p, bias, lengths, c_save, T (>= 1), B, H, dtype   as in the run
+ *   dh       device [T][B][H], dtype: gradient of h_out (past a sequence's length
+ *            not looked at)
+ *   dc_out   device fp32 [B][H] or NULL (zeros): gradient of c_out
+ *   dp       device [T][B][4H], dtype: gradient of p (zero past the length)
+ *   dc0      device fp32 [B][H] or NULL: gradient of c0; may be dc_out itself
+ *   dbias    device fp32 [4H] or NULL: gradient of bias (the sum of dp, before its
+ *            rounding, over timesteps and sequences)
+ *   workspace   as for the run, for backward = 1 (2 when dbias is not NULL)
+ * dp must not overlap the other arrays.
+ *
+ * approx_lstm_linear_workspace -- bytes of workspace of a run (backward = 0), of
+ * a backward pass without (1) or with dbias (2) on the current device.
+ *
+ * Long sequences are spread over workgroups that hand states on.  They take their
+ * places in the order in which they start, so nobody waits for one that has not
+ * started; should a (bounded) wait run out all the same, what depends on it is NaN.
+ *
+ * Errors: INVALID_ARG for a null p, h_out, dh, c_save (backward) or dp, sizes
+ * below those above, a dtype that is neither 0 nor 1, a pointer not aligned to its
+ * elements, a workspace missing, too small or not aligned; UNSUPPORTED for a
+ * row of B sequences (4 B H elements) of 2 GiB or more.
+ */
+#define APPROX_LSTM_LINEAR_SAVE 8
+
+approx_lstm_status approx_lstm_linear_run(const void* p, const float* bias, int32_t T, int32_t B, int32_t H,
+                                          int32_t dtype, const int32_t* lengths, const float* c0, void* h_out,
+                                          float* c_out, float* c_save, void* workspace, uint64_t workspace_bytes,
+                                          void* hip_stream);
+approx_lstm_status approx_lstm_linear_backward(const void* p, const float* bias, int32_t T, int32_t B, int32_t H,
+                                               int32_t dtype, const int32_t* lengths, const float* c_save,
+                                               const void* dh, const float* dc_out, void* dp, float* dc0,
+                                               float* dbias, void* workspace, uint64_t workspace_bytes,
+                                               void* hip_stream);
+approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H, int32_t backward, uint64_t* bytes);
+
+/*
+ * Gate products with 4-bit weights -- the other way to make a gate matrix small:
+ * every weight a 4-bit level, with one scale s and one zero level z for each
+ * group of G neighbouring columns of a row,
+ *
+ *     y[n][r] = bias[r] + sum_d s[r][d / G] (q[r][d] - z[r][d / G]) x[n][d].
+ *
+ * approx_lstm_q4_prepare -- round a matrix to levels and lay it out on the
+ * current device.  w host fp32 [rows][cols] (finite), for instance W_ih (rows =
+ * 4H, cols = D).  Per group: lo = min(0, min w), hi = max(0, max w), s = (hi - lo) /
+ * 15 rounded to fp32, z = -lo / s and q = w / s + z rounded to the nearest level in
+ * 0 .. 15.
+ * approx_lstm_q4_load -- lay out levels that the caller has: q device
+ * [rows][ceil(cols / 2)] bytes, column d in the low half of byte d / 2 for even d,
+ * else in the high half; scale device fp32 [rows][ceil(cols / G)]; zero device
+ * uint8 [rows][ceil(cols / G)], each at most 15 (else INVALID_ARG), or NULL: 8
+ * everywhere.
+ *   rows, cols   at least 1
+ *   group        G: 32, 64 or 128 (the last group of a row may be cut short)
+ * Both synchronise hip_stream; the arrays may be freed afterwards.
+ * approx_lstm_q4_get -- the stored matrix as host arrays in the formats of
+ * approx_lstm_q4_load (any may be NULL); synchronises hip_stream.
+ *
+ * approx_lstm_q4_run -- y = the product with x device [N][cols] plus bias (device
+ * fp32 [rows], or NULL), y device [N][rows].  x and y hold `dtype` (0 = fp32, 1 =
+ * bf16), sums are fp32; the levels enter exactly and scales as fp32, so nothing is
+ * rounded but the sums and, for bf16, y.  N >= 0 (0: nothing is done).  A row of x
+ * that holds an infinity or a NaN leaves infinities or NaN in its row of y, in no
+ * other.
+ * Asynchronous on hip_stream, allocates nothing, can be captured; a matrix is
+ * never written by a run, so runs may overlap.  x and y must not overlap.
+ *
+ * Errors: INVALID_ARG for a null m, x or y, sizes below those above, another
+ * dtype or group, a pointer not aligned to its elements, weights that are not
+ * finite, a zero level above 15.
+ */
+typedef struct approx_lstm_q4 approx_lstm_q4;   /* opaque */
+
+approx_lstm_status approx_lstm_q4_prepare(const float* w, int32_t rows, int32_t cols, int32_t group,
+                                          void* hip_stream, approx_lstm_q4** out);
+approx_lstm_status approx_lstm_q4_load(const uint8_t* q, const float* scale, const uint8_t* zero, int32_t rows,
+                                       int32_t cols, int32_t group, void* hip_stream, approx_lstm_q4** out);
+approx_lstm_status approx_lstm_q4_get(const approx_lstm_q4* m, uint8_t* q, float* scale, uint8_t* zero,
+                                      void* hip_stream);
+approx_lstm_status approx_lstm_q4_run(const approx_lstm_q4* m, const void* x, int32_t N, int32_t dtype,
+                                      const float* bias, void* y, void* hip_stream);
+void approx_lstm_q4_destroy(approx_lstm_q4* m);
+
 /* approx_lstm_destroy -- free the model and its device memory (NULL is a no-op). */
 void approx_lstm_destroy(approx_lstm_model* m);
 

@@ -86,6 +86,16 @@ _sigs = {
     "approx_lstm_exact_set_launch": [_vp, _i32],
     "approx_lstm_exact_set_start_wait": [_vp, ctypes.c_double],
 }
+_sigs.update({
+    "approx_lstm_linear_run": [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_uint64, _vp],
+    "approx_lstm_linear_backward": [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    ctypes.c_uint64, _vp],
+    "approx_lstm_linear_workspace": [_i32, _i32, _i32, _i32, _vp],
+    "approx_lstm_q4_prepare": [_vp, _i32, _i32, _i32, _vp, ctypes.POINTER(_vp)],
+    "approx_lstm_q4_load": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, ctypes.POINTER(_vp)],
+    "approx_lstm_q4_get": [_vp, _vp, _vp, _vp, _vp],
+    "approx_lstm_q4_run": [_vp, _vp, _i32, _i32, _vp, _vp, _vp],
+})
 for _name, _args in _sigs.items():
     getattr(lib, _name).argtypes = _args
     getattr(lib, _name).restype = ctypes.c_int
@@ -93,6 +103,8 @@ lib.approx_lstm_destroy.argtypes = [_vp]
 lib.approx_lstm_destroy.restype = None
 lib.approx_lstm_exact_destroy.argtypes = [_vp]
 lib.approx_lstm_exact_destroy.restype = None
+lib.approx_lstm_q4_destroy.argtypes = [_vp]
+lib.approx_lstm_q4_destroy.restype = None
 lib.approx_lstm_last_error.argtypes = []
 lib.approx_lstm_last_error.restype = ctypes.c_char_p
 
@@ -397,3 +409,191 @@ def approx_lstm_exact_set_launch(model, blocks):
 
 def approx_lstm_exact_set_start_wait(model, wait_us):
     return _check(lib.approx_lstm_exact_set_start_wait(model.handle, float(wait_us)))
+
+
+LINEAR_SAVE = 8   # timesteps between two states of c_save
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _on(t, name, shape, dtype, device, optional=False):
+    """Device pointer of a contiguous tensor of that shape and type on `device`."""
+    if t is None:
+        if optional:
+            return None
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous {dtype}".replace("torch.", ""))
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t.data_ptr()
+
+
+class _Launch:
+    """The device of a call's tensors made current, its stream, and workspace
+    from the caller or, for the length of the call, from torch's allocator."""
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.before = device, stream, None
+
+    def __enter__(self):
+        if self.device.index != torch.cuda.current_device():
+            self.before = torch.cuda.current_device()
+            torch.cuda.set_device(self.device)
+        self.handle = _stream(self.stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+
+    def workspace(self, given, T, B, H, backward):
+        """(tensor or None, pointer, bytes) for a call of these sizes."""
+        if given is not None:
+            if not isinstance(given, torch.Tensor) or not given.is_cuda or not given.is_contiguous():
+                raise TypeError("workspace must be a contiguous torch tensor on the GPU")
+            if given.device != self.device:
+                raise ValueError(f"workspace is on {given.device}, not on {self.device}")
+            return given, given.data_ptr(), given.numel() * given.element_size()
+        n = _linear_workspace(T, B, H, backward)
+        if not n:
+            return None, None, 0
+        if self.handle == torch.cuda.current_stream().cuda_stream:
+            t = torch.empty(n, dtype=torch.uint8, device=self.device)
+        else:   # from the pool of the stream that uses it
+            with torch.cuda.stream(torch.cuda.ExternalStream(self.handle, device=self.device)):
+                t = torch.empty(n, dtype=torch.uint8, device=self.device)
+        return t, t.data_ptr(), n
+
+
+def _linear_workspace(T, B, H, backward):
+    n = ctypes.c_uint64()
+    _check(lib.approx_lstm_linear_workspace(T, B, H, backward, ctypes.byref(n)))
+    return n.value
+
+
+def _gates(p):
+    """(T, B, H, device, dtype code) of pre-activations p [T, B, 4H]."""
+    if not isinstance(p, torch.Tensor) or not p.is_cuda:
+        raise TypeError("p must be a torch tensor on the GPU")
+    if p.dtype not in _DTYPES or not p.is_contiguous():
+        raise TypeError("p must be contiguous float32 or bfloat16")
+    if p.dim() != 3 or p.shape[2] % 4 or not p.shape[2]:
+        raise ValueError(f"p has shape {tuple(p.shape)}, expected (T, B, 4 H)")
+    return p.shape[0], p.shape[1], p.shape[2] // 4, p.device, _DTYPES[p.dtype]
+
+
+def approx_lstm_linear_run(p, h_out, bias=None, lengths=None, c0=None, c_out=None, c_save=None, workspace=None,
+                           stream=None):
+    """Gated linear recurrence.  p [T, B, 4H], h_out [T, B, H] GPU float32 or
+    bfloat16; bias [4H], c0, c_out [B, H], c_save [ceil(T / 8), B, H] float32,
+    lengths [B] int32, or None.  workspace: a GPU tensor of at least
+    approx_lstm_linear_workspace(T, B, H) bytes, or None (taken from torch)."""
+    T, B, H, dev, dt = _gates(p)
+    f32 = torch.float32
+    with _Launch(dev, stream) as call:
+        ws, wp, wn = call.workspace(workspace, T, B, H, 0)
+        st = lib.approx_lstm_linear_run(
+            p.data_ptr(), _on(bias, "bias", (4 * H,), f32, dev, True), T, B, H, dt,
+            _on(lengths, "lengths", (B,), torch.int32, dev, True), _on(c0, "c0", (B, H), f32, dev, True),
+            _on(h_out, "h_out", (T, B, H), p.dtype, dev), _on(c_out, "c_out", (B, H), f32, dev, True),
+            _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, dev, True), wp, wn, call.handle)
+    return _check(st)
+
+
+def approx_lstm_linear_backward(p, dh, c_save, dp, bias=None, lengths=None, dc_out=None, dc0=None, dbias=None,
+                                workspace=None, stream=None):
+    """Gradients of the gated linear recurrence: dp [T, B, 4H], dc0 [B, H] and
+    dbias [4H] (None: not wanted) from dh [T, B, H] and dc_out [B, H] (None:
+    zeros), with the run's p, bias, lengths and c_save."""
+    T, B, H, dev, dt = _gates(p)
+    f32 = torch.float32
+    with _Launch(dev, stream) as call:
+        ws, wp, wn = call.workspace(workspace, T, B, H, 1 if dbias is None else 2)
+        st = lib.approx_lstm_linear_backward(
+            p.data_ptr(), _on(bias, "bias", (4 * H,), f32, dev, True), T, B, H, dt,
+            _on(lengths, "lengths", (B,), torch.int32, dev, True),
+            _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, dev),
+            _on(dh, "dh", (T, B, H), p.dtype, dev), _on(dc_out, "dc_out", (B, H), f32, dev, True),
+            _on(dp, "dp", (T, B, 4 * H), p.dtype, dev), _on(dc0, "dc0", (B, H), f32, dev, True),
+            _on(dbias, "dbias", (4 * H,), f32, dev, True), wp, wn, call.handle)
+    return _check(st)
+
+
+def approx_lstm_linear_workspace(T, B, H, backward=0, device=None):
+    """Bytes of workspace of a run (backward 0) or of a backward pass without (1)
+    or with dbias (2), on `device` (None: the current one)."""
+    with _Launch(torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device), 0):
+        return _linear_workspace(int(T), int(B), int(H), int(backward))
+
+
+class Q4Matrix:
+    """Owning handle of an approx_lstm_q4 (a matrix of 4-bit levels)."""
+
+    def __init__(self, handle, rows, cols, group, device):
+        self.handle = handle
+        self.rows, self.cols, self.group, self.device = rows, cols, group, device
+
+    def __del__(self, _destroy=lib.approx_lstm_q4_destroy):
+        h, self.handle = getattr(self, "handle", None), None
+        if h:
+            _destroy(h)
+
+
+def approx_lstm_q4_prepare(w, group=128, stream=None):
+    """Host float32 matrix w [rows, cols] rounded to 4-bit levels with a scale and
+    a zero level per `group` columns; returns a Q4Matrix on the current device."""
+    w, wp = _host(w, np.float32)
+    if w.ndim != 2:
+        raise ValueError(f"w has shape {w.shape}, expected (rows, cols)")
+    out = ctypes.c_void_p()
+    _check(lib.approx_lstm_q4_prepare(wp, *w.shape, int(group), _stream(stream), ctypes.byref(out)))
+    return Q4Matrix(out.value, *w.shape, int(group), torch.device("cuda", torch.cuda.current_device()))
+
+
+def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):
+    """Levels q [rows, ceil(cols / 2)] uint8 (two in a byte, even columns in the
+    low half), scale [rows, ceil(cols / group)] float32 and zero, as scale, uint8
+    (None: 8): GPU tensors; returns a Q4Matrix."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 2:
+        raise TypeError("q must be a torch tensor [rows, ceil(cols / 2)] on the GPU")
+    cols, group = int(cols), int(group)
+    rows, dev, groups = q.shape[0], q.device, -(-cols // group) if group > 0 else 0
+    out = ctypes.c_void_p()
+    with _Launch(dev, stream) as call:
+        _check(lib.approx_lstm_q4_load(
+            _on(q, "q", (rows, (cols + 1) // 2), torch.uint8, dev),
+            _on(scale, "scale", (rows, groups), torch.float32, dev),
+            _on(zero, "zero", (rows, groups), torch.uint8, dev, True), rows, cols, group, call.handle,
+            ctypes.byref(out)))
+    return Q4Matrix(out.value, rows, cols, group, dev)
+
+
+def approx_lstm_q4_get(m, stream=None):
+    """The stored levels, scales and zero levels as host arrays in the formats of
+    approx_lstm_q4_load."""
+    groups = -(-m.cols // m.group)
+    q = np.empty((m.rows, (m.cols + 1) // 2), np.uint8)
+    s = np.empty((m.rows, groups), np.float32)
+    z = np.empty((m.rows, groups), np.uint8)
+    with _Launch(m.device, stream) as call:
+        _check(lib.approx_lstm_q4_get(m.handle, q.ctypes.data, s.ctypes.data, z.ctypes.data, call.handle))
+    return dict(q=q, scale=s, zero=z)
+
+
+def approx_lstm_q4_run(m, x, y, bias=None, stream=None):
+    """y [N, rows] = x [N, cols] times the matrix plus bias [rows] (float32 or
+    None); x and y GPU float32 or bfloat16."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2:
+        raise TypeError("x must be a torch tensor [N, cols] on the GPU")
+    if x.dtype not in _DTYPES:
+        raise TypeError("x must be float32 or bfloat16")
+    N, dev = x.shape[0], m.device
+    with _Launch(dev, stream) as call:
+        st = lib.approx_lstm_q4_run(
+            m.handle, _on(x, "x", (N, m.cols), x.dtype, dev), N, _DTYPES[x.dtype],
+            _on(bias, "bias", (m.rows,), torch.float32, dev, True), _on(y, "y", (N, m.rows), x.dtype, dev), call.handle)
+    return _check(st)

@@ -17,6 +17,7 @@
 
 #include "../../include/approx_lstm.h"
 #include "factorise.hpp"
+#include "gated.hpp"
 #include "kernels.hpp"
 
 namespace {
@@ -1692,5 +1693,248 @@ approx_lstm_status approx_lstm_exact_set_start_wait(approx_lstm_exact* m, double
 }
 
 void approx_lstm_exact_destroy(approx_lstm_exact* m) { delete m; }
+
+}  // extern "C"
+
+// Gated linear recurrence (linear.hip) and 4-bit gate products (q4.hip).
+namespace {
+
+approx_lstm_status current_cus(int* num_cu) {
+  int dev = 0;
+  HIP_TRY(hipGetDevice(&dev), "hipGetDevice");
+  HIP_TRY(hipDeviceGetAttribute(num_cu, hipDeviceAttributeMultiprocessorCount, dev), "hipDeviceGetAttribute");
+  return APPROX_LSTM_OK;
+}
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// Checks what a run and a backward pass have in common, and fills a's num_cu.
+approx_lstm_status check_linear(alstm::LinearArgs& a, int dtype, int backward, const void* ws, uint64_t ws_bytes) {
+  if (a.B < 1 || a.H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need B >= 1 and H >= 1");
+  if (dtype != 0 && dtype != 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "dtype = %d is neither 0 nor 1", dtype);
+  const size_t el = dtype ? 2 : 4;
+  if ((uint64_t)a.B * a.H * 4 * el >= (1ull << 31))
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "B = %d, H = %d: a timestep of 2 GiB or more", a.B, a.H);
+  for (const void* p : {a.p, (const void*)a.h, a.dh, (const void*)a.dp})
+    if (!aligned(p, el)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "p, h or a gradient not aligned to its elements");
+  for (const void* p : {(const void*)a.bias, (const void*)a.lengths, (const void*)a.c0, (const void*)a.c_out,
+                        (const void*)a.c_save, (const void*)a.dc_out, (const void*)a.dc0, (const void*)a.dbias})
+    if (!aligned(p, 4)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "a state, bias, gradient or lengths not aligned to 4 bytes");
+  a.bf16 = dtype;
+  approx_lstm_status st = current_cus(&a.num_cu);
+  if (st != APPROX_LSTM_OK) return st;
+  const size_t need = alstm::linear_workspace(a.T, a.B, a.H, a.num_cu, backward);
+  if (need && (!ws || ws_bytes < need || !aligned(ws, 16)))
+    return fail(APPROX_LSTM_ERR_INVALID_ARG, "workspace of %zu bytes, 16-byte aligned, needed (given: %llu)", need,
+                (unsigned long long)(ws ? ws_bytes : 0));
+  return APPROX_LSTM_OK;
+}
+
+}  // namespace
+
+struct approx_lstm_q4 {
+  alstm::Q4Matrix m{};
+  int device = -1, num_cu = 0;
+  uint8_t* d_store = nullptr;
+
+  ~approx_lstm_q4() {
+    if (device < 0) return;
+    DeviceScope ds(device);
+    dfree(d_store);
+  }
+};
+
+extern "C" {
+
+approx_lstm_status approx_lstm_linear_run(const void* p, const float* bias, int32_t T, int32_t B, int32_t H,
+                                          int32_t dtype, const int32_t* lengths, const float* c0, void* h_out,
+                                          float* c_out, float* c_save, void* workspace, uint64_t workspace_bytes,
+                                          void* hip_stream) {
+  g_last_error.clear();
+  if (T < 0) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 0");
+  if (T > 0 && (!p || !h_out)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null p or h_out");
+  alstm::LinearArgs a{};
+  a.p = p; a.bias = bias; a.T = T; a.B = B; a.H = H; a.lengths = lengths;
+  a.c0 = c0; a.h = h_out; a.c_out = c_out; a.c_save = c_save;
+  approx_lstm_status st = check_linear(a, dtype, 0, workspace, workspace_bytes);
+  if (st != APPROX_LSTM_OK) return st;
+  HIP_TRY(alstm::launch_linear(a, workspace, (hipStream_t)hip_stream), "launch gated linear recurrence");
+  return APPROX_LSTM_OK;
+}
+
+approx_lstm_status approx_lstm_linear_backward(const void* p, const float* bias, int32_t T, int32_t B, int32_t H,
+                                               int32_t dtype, const int32_t* lengths, const float* c_save,
+                                               const void* dh, const float* dc_out, void* dp, float* dc0,
+                                               float* dbias, void* workspace, uint64_t workspace_bytes,
+                                               void* hip_stream) {
+  g_last_error.clear();
+  if (T < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 1");
+  if (!p || !c_save || !dh || !dp) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null p, c_save, dh or dp");
+  alstm::LinearArgs a{};
+  a.p = p; a.bias = bias; a.T = T; a.B = B; a.H = H; a.lengths = lengths;
+  a.c_save = const_cast<float*>(c_save);
+  a.dh = dh; a.dc_out = dc_out; a.dp = dp; a.dc0 = dc0; a.dbias = dbias;
+  approx_lstm_status st = check_linear(a, dtype, dbias ? 2 : 1, workspace, workspace_bytes);
+  if (st != APPROX_LSTM_OK) return st;
+  HIP_TRY(alstm::launch_linear_backward(a, workspace, (hipStream_t)hip_stream), "launch gated linear backward pass");
+  return APPROX_LSTM_OK;
+}
+
+approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H, int32_t backward, uint64_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null bytes");
+  if (T < 0 || B < 1 || H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 0, B >= 1 and H >= 1");
+  if (backward < 0 || backward > 2) return fail(APPROX_LSTM_ERR_INVALID_ARG, "backward = %d not in 0..2", backward);
+  int num_cu = 0;
+  approx_lstm_status st = current_cus(&num_cu);
+  if (st != APPROX_LSTM_OK) return st;
+  *bytes = alstm::linear_workspace(T, B, H, num_cu, backward);
+  return APPROX_LSTM_OK;
+}
+
+approx_lstm_status approx_lstm_q4_load(const uint8_t* q, const float* scale, const uint8_t* zero, int32_t rows,
+                                       int32_t cols, int32_t group, void* hip_stream, approx_lstm_q4** out) {
+  g_last_error.clear();
+  if (!q || !scale || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
+  if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (group != 32 && group != 64 && group != 128)
+    return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
+  if (!aligned(scale, 4)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "scale not aligned to 4 bytes");
+  approx_lstm_q4* m = new (std::nothrow) approx_lstm_q4();
+  if (!m) return fail(APPROX_LSTM_ERR_OUT_OF_MEMORY, "host allocation failed");
+  hipStream_t stream = (hipStream_t)hip_stream;
+  approx_lstm_status st = APPROX_LSTM_OK;
+  auto step = [&](hipError_t e, const char* what) {
+    if (st == APPROX_LSTM_OK && e != hipSuccess) st = hip_fail(e, what);
+  };
+  step(hipGetDevice(&m->device), "hipGetDevice");
+  if (st == APPROX_LSTM_OK) st = current_cus(&m->num_cu);
+  m->m.R = rows; m->m.D = cols; m->m.G = group; m->m.groups = (cols + group - 1) / group;
+  const size_t bytes = alstm::q4_bytes(rows, cols, group);
+  if (st == APPROX_LSTM_OK) step(hipMalloc(&m->d_store, bytes + 256), "hipMalloc(levels)");
+  if (st == APPROX_LSTM_OK) {
+    alstm::q4_place(m->m, m->d_store);
+    int* bad = reinterpret_cast<int*>(m->d_store + bytes);
+    int host_bad = 0;
+    step(alstm::launch_clear_u64(reinterpret_cast<unsigned long long*>(bad), 1, stream), "clear");
+    step(alstm::launch_q4_layout(m->m, q, scale, zero, bad, stream), "launch q4_layout_kernel");
+    step(hipMemcpyAsync(&host_bad, bad, sizeof host_bad, hipMemcpyDeviceToHost, stream), "read the check of the levels");
+    step(hipStreamSynchronize(stream), "hipStreamSynchronize");
+    if (st == APPROX_LSTM_OK && host_bad) st = fail(APPROX_LSTM_ERR_INVALID_ARG, "a zero level is above 15");
+  }
+  if (st != APPROX_LSTM_OK) {
+    delete m;
+    return st;
+  }
+  *out = m;
+  return APPROX_LSTM_OK;
+}
+
+approx_lstm_status approx_lstm_q4_prepare(const float* w, int32_t rows, int32_t cols, int32_t group,
+                                          void* hip_stream, approx_lstm_q4** out) {
+  g_last_error.clear();
+  if (!w || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
+  if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (group != 32 && group != 64 && group != 128)
+    return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
+  const size_t R = rows, D = cols, groups = (D + group - 1) / group, row_bytes = (D + 1) / 2;
+  std::vector<uint8_t> q, z;
+  std::vector<float> s;
+  try {
+    q.assign(R * row_bytes, 0);
+    z.resize(R * groups);
+    s.resize(R * groups);
+  } catch (const std::bad_alloc&) {
+    return fail(APPROX_LSTM_ERR_OUT_OF_MEMORY, "host allocation failed");
+  }
+  for (size_t r = 0; r < R; ++r)
+    for (size_t g = 0; g < groups; ++g) {
+      const size_t d0 = g * group, d1 = std::min(D, d0 + group);
+      double lo = 0.0, hi = 0.0;
+      for (size_t d = d0; d < d1; ++d) {
+        const float v = w[r * D + d];
+        if (!std::isfinite(v)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "w[%zu][%zu] is not finite", r, d);
+        lo = std::min(lo, (double)v);
+        hi = std::max(hi, (double)v);
+      }
+      const float sf = (float)((hi - lo) / 15.0);
+      const double sd = sf > 0.f ? (double)sf : 1.0;   // all zeros: any level does
+      const double zd = std::min(15.0, std::max(0.0, std::nearbyint(-lo / sd)));
+      s[r * groups + g] = sf;
+      z[r * groups + g] = (uint8_t)zd;
+      for (size_t d = d0; d < d1; ++d) {
+        const double v = std::min(15.0, std::max(0.0, std::nearbyint((double)w[r * D + d] / sd + zd)));
+        q[r * row_bytes + d / 2] |= (uint8_t)((unsigned)v << (4 * (d & 1)));
+      }
+    }
+  hipStream_t stream = (hipStream_t)hip_stream;
+  uint8_t* d_q = nullptr;
+  float* d_s = nullptr;
+  uint8_t* d_z = nullptr;
+  approx_lstm_status st = APPROX_LSTM_OK;
+  auto step = [&](hipError_t e, const char* what) {
+    if (st == APPROX_LSTM_OK && e != hipSuccess) st = hip_fail(e, what);
+  };
+  auto up = [&](auto*& dst, const auto& src, const char* what) {
+    const size_t n = src.size() * sizeof(src[0]);
+    step(hipMalloc(&dst, n), what);
+    if (st == APPROX_LSTM_OK) step(hipMemcpyAsync(dst, src.data(), n, hipMemcpyHostToDevice, stream), what);
+  };
+  up(d_q, q, "levels");
+  up(d_s, s, "scales");
+  up(d_z, z, "zero levels");
+  if (st == APPROX_LSTM_OK) st = approx_lstm_q4_load(d_q, d_s, d_z, rows, cols, group, hip_stream, out);
+  else (void)hipStreamSynchronize(stream);   // no copy may outlive the vectors
+  dfree(d_q);
+  dfree(d_s);
+  dfree(d_z);
+  return st;
+}
+
+approx_lstm_status approx_lstm_q4_get(const approx_lstm_q4* m, uint8_t* q, float* scale, uint8_t* zero,
+                                      void* hip_stream) {
+  g_last_error.clear();
+  if (!m) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null matrix");
+  DeviceScope ds(m->device);
+  if (!ds.ok) return fail(APPROX_LSTM_ERR_DEVICE, "cannot select the matrix's device");
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const size_t nq = (size_t)m->m.R * ((m->m.D + 1) / 2), ns = (size_t)m->m.R * m->m.groups;
+  uint8_t* tmp = nullptr;
+  HIP_TRY(hipMalloc(&tmp, 5 * ns + nq), "hipMalloc(levels)");
+  float* t_s = reinterpret_cast<float*>(tmp);
+  uint8_t* t_z = tmp + 4 * ns;
+  uint8_t* t_q = t_z + ns;
+  approx_lstm_status st = APPROX_LSTM_OK;
+  auto step = [&](hipError_t e, const char* what) {
+    if (st == APPROX_LSTM_OK && e != hipSuccess) st = hip_fail(e, what);
+  };
+  step(alstm::launch_q4_unpack(m->m, t_q, t_s, t_z, stream), "launch q4_unpack_kernel");
+  if (q) step(hipMemcpyAsync(q, t_q, nq, hipMemcpyDeviceToHost, stream), "levels");
+  if (scale) step(hipMemcpyAsync(scale, t_s, ns * 4, hipMemcpyDeviceToHost, stream), "scales");
+  if (zero) step(hipMemcpyAsync(zero, t_z, ns, hipMemcpyDeviceToHost, stream), "zero levels");
+  const hipError_t done = hipStreamSynchronize(stream);   // (in any case: no copy may outlive the call)
+  step(done, "hipStreamSynchronize");
+  dfree(tmp);
+  return st;
+}
+
+approx_lstm_status approx_lstm_q4_run(const approx_lstm_q4* m, const void* x, int32_t N, int32_t dtype,
+                                      const float* bias, void* y, void* hip_stream) {
+  g_last_error.clear();
+  if (!m) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null matrix");
+  if (N < 0) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need N >= 0");
+  if (dtype != 0 && dtype != 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "dtype = %d is neither 0 nor 1", dtype);
+  if (N == 0) return APPROX_LSTM_OK;
+  if (!x || !y) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null x or y");
+  const size_t el = dtype ? 2 : 4;
+  if (!aligned(x, el) || !aligned(y, el) || !aligned(bias, 4))
+    return fail(APPROX_LSTM_ERR_INVALID_ARG, "x, y or bias not aligned to its elements");
+  DeviceScope ds(m->device);
+  if (!ds.ok) return fail(APPROX_LSTM_ERR_DEVICE, "cannot select the matrix's device");
+  HIP_TRY(alstm::launch_q4(m->m, x, N, dtype, bias, y, m->num_cu, (hipStream_t)hip_stream), "launch q4 product");
+  return APPROX_LSTM_OK;
+}
+
+void approx_lstm_q4_destroy(approx_lstm_q4* m) { delete m; }
 
 }  // extern "C"

@@ -1,0 +1,63 @@
+// Internal interface of the gated linear recurrence (linear.hip) and the
+// 4-bit gate products (q4.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstddef>
+#include <cstdint>
+
+namespace alstm {
+
+constexpr int kLinearSave = 8;     // timesteps between two saved states
+
+// A gated linear recurrence, forward or back.  Layouts (row-major): p, dp
+// [T][B][4H] (gate rows i, f, g, o), h, dh [T][B][H] of the call's type; c0,
+// c_out, dc_out, dc0 [B][H], c_save [ceil(T/8)][B][H], bias, dbias [4H] fp32.
+struct LinearArgs {
+  const void* p;
+  const float* bias;      // or null
+  const int* lengths;     // [B] or null
+  const float* c0;        // or null
+  void* h;
+  float* c_out;           // or null
+  float* c_save;          // run: or null (written); backward: read
+  const void* dh;
+  const float* dc_out;    // or null
+  void* dp;
+  float* dc0;             // or null
+  float* dbias;           // or null
+  int T, B, H;
+  int bf16;               // 1: p, h and their gradients hold bf16, else fp32
+  int num_cu;
+  // workspace (linear_workspace)
+  float* dpart;           // [rows][4H]: sums of dp, one row per sequence (and stretch of time)
+};
+
+// Bytes of workspace of a run (backward 0), a backward pass (1) or one with the
+// bias gradient (2).
+size_t linear_workspace(int T, int B, int H, int num_cu, int backward);
+// Launches the recurrence, or its backward pass, with that workspace.
+hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
+hipError_t launch_linear_backward(const LinearArgs& a, void* ws, hipStream_t stream);
+
+// A matrix of 4-bit levels (q4.hip).
+struct Q4Matrix {
+  uint8_t* q;         // [R][ceil(D/2)]
+  float* s;           // [R][groups]
+  float* z;           // [R][groups]
+  int R, D, G, groups;
+};
+// Bytes of device memory of a matrix, and its arrays' places there.
+size_t q4_bytes(int R, int D, int G);
+void q4_place(Q4Matrix& m, uint8_t* store);
+// Lays out q [R][ceil(D/2)], scale [R][groups], zero [R][groups] (null: 8) in m;
+// *bad becomes 1 where a zero level is above 15.
+hipError_t launch_q4_layout(const Q4Matrix& m, const uint8_t* q, const float* scale, const uint8_t* zero, int* bad,
+                            hipStream_t stream);
+// The opposite: the matrix in the formats of its layout's arguments.
+hipError_t launch_q4_unpack(const Q4Matrix& m, uint8_t* q, float* scale, uint8_t* zero, hipStream_t stream);
+// y [N][R] = x [N][D] times the matrix, plus bias [R] (or null).
+hipError_t launch_q4(const Q4Matrix& m, const void* x, int N, int bf16, const float* bias, void* y, int num_cu,
+                     hipStream_t stream);
+
+}  // namespace alstm

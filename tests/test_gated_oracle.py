@@ -1,0 +1,154 @@
+"""Pins of the float64 oracles of the gated linear recurrence and of the 4-bit
+gate product, and the refusals of their entry points (no GPU)."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import gated
+from paper_1905_00689_amd import binding as B
+
+P = ctypes.c_void_p(4096)      # an address that no refused call looks at
+ODD = ctypes.c_void_p(4097)
+
+
+def inputs(T, Bn, H, seed=1):
+    r = np.random.default_rng([190500689, seed])
+    return dict(p=r.normal(size=(T, Bn, 4 * H)), bias=r.normal(size=4 * H), c0=r.normal(size=(Bn, H)),
+                lengths=r.integers(0, T + 1, Bn), dh=r.normal(size=(T, Bn, H)), dc=r.normal(size=(Bn, H)))
+
+
+def test_recurrence_is_an_lstm_without_recurrent_weights():
+    a = inputs(9, 3, 5)
+    m = torch.nn.LSTM(20, 5).double()
+    with torch.no_grad():
+        m.weight_ih_l0.copy_(torch.eye(20))
+        m.weight_hh_l0.zero_()
+        m.bias_ih_l0.copy_(torch.from_numpy(a["bias"]))
+        m.bias_hh_l0.zero_()
+        ht, (_, ct) = m(torch.from_numpy(a["p"]), (torch.zeros(1, 3, 5).double(), torch.from_numpy(a["c0"])[None]))
+    h, c, _, _ = gated.linear_lstm(a["p"], a["bias"], None, a["c0"])
+    np.testing.assert_allclose(h, ht.numpy(), atol=1e-12)
+    np.testing.assert_allclose(c[-1], ct[0].numpy(), atol=1e-12)
+
+
+def test_lengths_stop_a_sequence():
+    a = inputs(7, 4, 3)
+    a["lengths"][:] = [0, 3, 7, 99]
+    h, c, _, _ = gated.linear_lstm(a["p"], a["bias"], a["lengths"], a["c0"])
+    assert np.array_equal(c[-1][0], a["c0"][0]) and not h[:, 0].any() and not h[3:, 1].any()
+    part, cp, _, _ = gated.linear_lstm(a["p"][:3, 1:2], a["bias"], None, a["c0"][1:2])
+    assert np.array_equal(h[:3, 1:2], part) and np.array_equal(c[-1][1:2], cp[-1])
+    whole, _, _, _ = gated.linear_lstm(a["p"], a["bias"], None, a["c0"])
+    assert np.array_equal(h[:, 2:], whole[:, 2:])
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_gradients_against_differences(ragged):
+    a = inputs(6, 2, 3, seed=2)
+    lengths = np.array([4, 0]) if ragged else None
+
+    def loss(p, b, c0):
+        h, c, _, _ = gated.linear_lstm(p, b, lengths, c0)
+        return (a["dh"] * h).sum() + (a["dc"] * c[-1]).sum()
+
+    got, _ = gated.linear_lstm_grad(a["p"], a["dh"], a["dc"], a["bias"], lengths, a["c0"])
+    step = 1e-6
+    for name, arr in (("dp", "p"), ("dbias", "bias"), ("dc0", "c0")):
+        num = np.zeros(a[arr].shape)
+        for k in np.ndindex(*a[arr].shape):
+            v = {n: a[n].copy() for n in ("p", "bias", "c0")}
+            v[arr][k] += step
+            up = loss(v["p"], v["bias"], v["c0"])
+            v[arr][k] -= 2 * step
+            num[k] = (up - loss(v["p"], v["bias"], v["c0"])) / (2 * step)
+        # central differences: step^2 of truncation, 1e-15 / step of rounding
+        np.testing.assert_allclose(got[name], num, atol=2e-8)
+
+
+@pytest.mark.parametrize("D,group", [(64, 32), (77, 32), (1, 128), (300, 128)])
+def test_levels_are_the_nearest(D, group):
+    w = np.random.default_rng(5).normal(size=(6, D)).astype(np.float32)
+    w[0] = 0.0
+    w[1] = np.abs(w[1])
+    q, s, z = gated.q4_round(w, group)
+    of = np.arange(D) // group
+    back = (q.astype(float) - z[:, of].astype(float)) * s[:, of]
+    # within half a step, and the rounding of the zero level by up to half a step more at the ends
+    assert (np.abs(back - w) <= s[:, of] * (1 + 1e-6)).all()
+    assert not back[0].any()
+    y, _ = gated.q4_product(q, s, z, group, np.eye(D))
+    np.testing.assert_allclose(y, back.T, atol=1e-12)
+    packed = gated.q4_pack(q)
+    assert packed.shape == (6, (D + 1) // 2) and np.array_equal(packed[:, 0] & 15, q[:, 0])
+
+
+def run_args(**over):
+    a = dict(p=P, bias=None, T=4, B=2, H=8, dtype=0, lengths=None, c0=None, h=P, c_out=None, c_save=None, ws=None,
+             n=0, stream=None)
+    a.update(over)
+    return list(a.values())
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(p=None), 1), (dict(h=None), 1), (dict(T=-1), 1), (dict(B=0), 1), (dict(H=0), 1), (dict(dtype=2), 1),
+    (dict(dtype=-1), 1), (dict(p=ODD), 1), (dict(h=ODD, dtype=1), 1), (dict(bias=ODD), 1), (dict(lengths=ODD), 1),
+    (dict(c0=ODD), 1), (dict(c_out=ODD), 1), (dict(c_save=ODD), 1), (dict(B=1 << 20, H=1 << 10), 6)])
+def test_run_refusals(over, status):
+    assert B.lib.approx_lstm_linear_run(*run_args(**over)) == status
+    assert B.approx_lstm_last_error()
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(p=None), 1), (dict(T=0), 1), (dict(B=0), 1), (dict(H=-3), 1), (dict(dtype=7), 1), (dict(c_save=None), 1),
+    (dict(dh=None), 1), (dict(dp=None), 1), (dict(dh=ODD), 1), (dict(dp=ODD), 1), (dict(dc_out=ODD), 1),
+    (dict(dc0=ODD), 1), (dict(dbias=ODD), 1), (dict(B=1 << 20, H=1 << 10), 6)])
+def test_backward_refusals(over, status):
+    a = dict(p=P, bias=None, T=4, B=2, H=8, dtype=0, lengths=None, c_save=P, dh=P, dc_out=None, dp=P, dc0=None,
+             dbias=None, ws=None, n=0, stream=None)
+    a.update(over)
+    assert B.lib.approx_lstm_linear_backward(*a.values()) == status
+
+
+def test_workspace_refusals():
+    n = ctypes.c_uint64()
+    for T, Bn, H, back, at in ((-1, 1, 1, 0, n), (1, 0, 1, 0, n), (1, 1, 0, 0, n), (1, 1, 1, 3, n), (1, 1, 1, 0, None)):
+        assert B.lib.approx_lstm_linear_workspace(T, Bn, H, back, None if at is None else ctypes.byref(at)) == 1
+
+
+@pytest.mark.parametrize("over", [dict(q=None), dict(scale=None), dict(rows=0), dict(cols=0), dict(group=16),
+                                  dict(group=0), dict(scale=ODD)])
+def test_load_refusals(over):
+    a = dict(q=P, scale=P, zero=None, rows=4, cols=64, group=32, stream=None)
+    a.update(over)
+    out = ctypes.c_void_p()
+    assert B.lib.approx_lstm_q4_load(*a.values(), ctypes.byref(out)) == 1 and not out.value
+
+
+def test_prepare_refusals():
+    out = ctypes.c_void_p()
+    w = np.ones((4, 64), np.float32)
+    ptr = w.ctypes.data
+    assert B.lib.approx_lstm_q4_prepare(None, 4, 64, 32, None, ctypes.byref(out)) == 1
+    assert B.lib.approx_lstm_q4_prepare(ptr, 0, 64, 32, None, ctypes.byref(out)) == 1
+    assert B.lib.approx_lstm_q4_prepare(ptr, 4, 64, 33, None, ctypes.byref(out)) == 1
+    for v in (np.inf, np.nan):
+        w[2, 5] = v
+        assert B.lib.approx_lstm_q4_prepare(ptr, 4, 64, 32, None, ctypes.byref(out)) == 1
+    assert "[2][5]" in B.approx_lstm_last_error() and not out.value
+
+
+def test_product_refuses_a_null_matrix():
+    assert B.lib.approx_lstm_q4_run(None, P, 1, 0, None, P, None) == 1
+    assert B.lib.approx_lstm_q4_get(None, None, None, None, None) == 1
+    B.lib.approx_lstm_q4_destroy(None)
+
+
+def test_tensors_on_the_host_are_refused():
+    t = torch.zeros(2, 1, 8)
+    with pytest.raises(TypeError):
+        B.approx_lstm_linear_run(t, torch.zeros(2, 1, 2))
+    with pytest.raises(TypeError):
+        B.approx_lstm_q4_load(torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(4, 1), None, 32, 32)

@@ -1,0 +1,299 @@
+"""The gated linear recurrence and its gradients against the float64 oracle,
+elementwise within its bounds on fp32 errors (and, for bf16 outputs, half a step
+of bf16: 2^-8 of the value)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import gated
+from paper_1905_00689_amd import binding as B
+
+from .gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+class Case:
+    """Inputs on the GPU (p, h and gradients `shift` elements into their buffers)
+    and, in float64, what the GPU was given."""
+
+    def __init__(self, T, Bn, H, dtype=F32, bias=True, state=True, lengths=None, seed=0, forget=2.0, shift=0, pad=None):
+        r = np.random.default_rng([190500689, seed, T, Bn, H])
+        self.T, self.B, self.H, self.dtype, self.shift = T, Bn, H, dtype, shift
+        p = r.normal(size=(T, Bn, 4 * H))
+        p[..., H:2 * H] += forget * r.random(H)
+        self.lengths = None if lengths is None else np.asarray(lengths, np.int32)
+        if pad is not None:
+            for b, n in enumerate(self.lengths):
+                p[max(0, int(n)):, b] = pad
+        self.p = self.place(p)
+        self.dh = self.place(r.normal(size=(T, Bn, H)))
+        if pad is not None:
+            for b, n in enumerate(self.lengths):
+                self.dh[max(0, int(n)):, b] = pad
+        f32 = lambda a: torch.from_numpy(a.astype(np.float32)).cuda()  # noqa: E731
+        self.bias = f32(r.normal(size=4 * H)) if bias else None
+        self.c0 = f32(r.normal(size=(Bn, H))) if state else None
+        self.dc = f32(r.normal(size=(Bn, H))) if state else None
+        self.len = None if lengths is None else torch.from_numpy(self.lengths).cuda()
+
+    def place(self, a):
+        t = torch.zeros(a.size + self.shift, dtype=self.dtype, device="cuda")
+        t[self.shift:] = torch.from_numpy(a.reshape(-1)).to(self.dtype).cuda()
+        return t[self.shift:].view(a.shape)
+
+    def empty(self, *shape):
+        t = torch.full((int(np.prod(shape)) + self.shift,), float("nan"), dtype=self.dtype, device="cuda")
+        return t[self.shift:].view(shape)
+
+    def out(self):
+        T, Bn, H = self.T, self.B, self.H
+        nan = lambda *s: torch.full(s, float("nan"), device="cuda")  # noqa: E731
+        return dict(h=self.empty(T, Bn, H), c=nan(Bn, H), save=nan(-(-T // 8), Bn, H), dp=self.empty(T, Bn, 4 * H),
+                    dc0=nan(Bn, H), db=nan(4 * H))
+
+    def run(self, o, **kw):
+        B.approx_lstm_linear_run(self.p, o["h"], bias=self.bias, lengths=self.len, c0=self.c0, c_out=o["c"],
+                                 c_save=o["save"], **kw)
+
+    def back(self, o, **kw):
+        B.approx_lstm_linear_backward(self.p, self.dh, o["save"], o["dp"], bias=self.bias, lengths=self.len,
+                                      dc_out=self.dc, dc0=o["dc0"], dbias=o["db"], **kw)
+
+    def host(self, t):
+        return None if t is None else t.double().cpu().numpy()
+
+    def want(self):
+        a = (self.host(self.bias), self.lengths, self.host(self.c0))
+        return (gated.linear_lstm(self.host(self.p), *a),
+                gated.linear_lstm_grad(self.host(self.p), self.host(self.dh), self.host(self.dc), *a))
+
+
+def near(name, got, want, bound, half):
+    got = got.double().cpu().numpy()
+    tol = bound * (1 + half) + half * np.abs(want) + 1e-30
+    worst = np.max(np.abs(got - want) / tol) if got.size else 0.0
+    assert np.isfinite(got).all() and worst <= 1.0, (name, worst)
+    return worst
+
+
+def check(k, o):
+    (h, c, he, ce), (g, ge) = k.want()
+    half = HALF[k.dtype]
+    said = [near("h", o["h"], h, he, half), near("c", o["c"], c[-1], ce[-1], HALF[F32]),
+            near("save", o["save"], c[:-1][::8], ce[:-1][::8], HALF[F32])]
+    said += [near("dp", o["dp"], g["dp"], ge["dp"], half), near("dc0", o["dc0"], g["dc0"], ge["dc0"], HALF[F32]),
+             near("dbias", o["db"], g["dbias"], ge["dbias"], HALF[F32])]
+    say("worst shares of the tolerances", *("%.2f" % v for v in said))
+
+
+SHAPES = [(1, 1, 1), (1, 5, 64), (2, 1, 3), (7, 3, 65), (8, 1, 128), (9, 2, 130), (17, 4, 31), (63, 1, 64),
+          (64, 2, 129), (65, 1, 2), (100, 1, 64), (129, 3, 50), (500, 2, 257), (2100, 1, 70), (4500, 1, 2)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,Bn,H", SHAPES)
+def test_run_and_gradients(T, Bn, H, dtype):
+    say("linear", T, Bn, H, dtype)
+    k = Case(T, Bn, H, dtype)
+    o = k.out()
+    k.run(o)
+    k.back(o)
+    check(k, o)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,H", [(40, 33), (200, 64), (1100, 20)])
+def test_lengths(T, H, dtype):
+    """Sequences of none, some and all timesteps (and lengths out of range); NaN
+    in the padding reaches nothing, and its outputs are zeros."""
+    n = [0, 1, T // 2, T - 1, T, T + 5, -3, 7]
+    say("lengths", T, H, dtype)
+    k = Case(T, len(n), H, dtype, lengths=n, pad=float("nan"))
+    o = k.out()
+    k.run(o)
+    k.back(o)
+    clean = Case(T, len(n), H, dtype, lengths=n, pad=0.0)
+    clean.p, clean.dh = torch.nan_to_num(k.p), torch.nan_to_num(k.dh)
+    check(clean, o)
+    for b, m in enumerate(n):
+        assert not o["h"][max(0, m):, b].any() and not o["dp"][max(0, m):, b].any()
+    assert torch.equal(o["c"][0], k.c0[0]) and torch.equal(o["dc0"][0], k.dc[0])
+
+
+@pytest.mark.parametrize("T", [1, 20, 300])
+def test_without_what_may_be_null(T):
+    say("nulls", T)
+    k = Case(T, 2, 34, bias=False, state=False)
+    o = k.out()
+    k.run(o)
+    k.back(o)
+    check(k, o)
+    h, dp = k.empty(T, 2, 4 * 34)[..., :34].contiguous(), o["dp"].clone()
+    B.approx_lstm_linear_run(k.p, h)
+    B.approx_lstm_linear_backward(k.p, k.dh, o["save"], dp)
+    assert torch.equal(h, o["h"]) and torch.equal(dp, o["dp"])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("H", [64, 35])
+def test_unaligned_rows_give_the_same_bits(H, dtype):
+    say("unaligned", H, dtype)
+    a, b = Case(150, 2, H, dtype), Case(150, 2, H, dtype, shift=1)
+    oa, ob = a.out(), b.out()
+    for k, o in ((a, oa), (b, ob)):
+        k.run(o)
+        k.back(o)
+    assert all(torch.equal(oa[n], ob[n]) for n in oa)
+
+
+@pytest.mark.parametrize("T,Bn,H", [(70, 2, 64), (1000, 1, 128)])
+def test_steps_and_pieces_join(T, Bn, H):
+    """A sequence in two pieces, and (its first timesteps) one token at a time
+    with the state updated in place, agrees with the whole within the bounds."""
+    say("pieces", T, Bn, H)
+    k = Case(T, Bn, H)
+    o = k.out()
+    k.run(o)
+    (h, c, he, ce), _ = k.want()
+    cut = T // 3
+    two, state = torch.empty_like(o["h"]), torch.empty_like(o["c"])
+    B.approx_lstm_linear_run(k.p[:cut].contiguous(), two[:cut], bias=k.bias, c0=k.c0, c_out=state)
+    B.approx_lstm_linear_run(k.p[cut:].contiguous(), two[cut:], bias=k.bias, c0=state, c_out=state)
+    near("h", two, h, he, HALF[F32])
+    near("c", state, c[-1], ce[-1], HALF[F32])
+    state = k.c0.clone()
+    for t in range(20):
+        B.approx_lstm_linear_run(k.p[t:t + 1], two[t:t + 1], bias=k.bias, c0=state, c_out=state)
+    near("h", two[:20], h[:20], he[:20], HALF[F32])
+
+
+def test_no_timesteps():
+    c0, c = torch.randn(3, 8, device="cuda"), torch.empty(3, 8, device="cuda")
+    p = torch.empty(0, 3, 32, device="cuda")
+    B.approx_lstm_linear_run(p, torch.empty(0, 3, 8, device="cuda"), c0=c0, c_out=c)
+    assert torch.equal(c, c0)
+    B.approx_lstm_linear_run(p, torch.empty(0, 3, 8, device="cuda"), c_out=c)
+    assert not c.any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 300])
+def test_gates_at_the_ends_of_their_range(T, dtype):
+    """Pre-activations of infinity and of the type's largest values close or open
+    a gate exactly: no NaN, no leak."""
+    say("ends", T, dtype)
+    big = torch.finfo(dtype).max
+    for v in (float("inf"), big, 200.0):
+        H = 16
+        p = torch.zeros(T, 1, 4, H, dtype=dtype, device="cuda")
+        p[:, :, 0] = -v          # i closed
+        p[:, :, 1] = v           # f open: the state stays
+        p[:, :, 2] = v
+        p[:, :, 3] = v           # o open
+        c0 = torch.linspace(-2, 2, H, device="cuda")[None].contiguous()
+        h, c = torch.empty(T, 1, H, dtype=dtype, device="cuda"), torch.empty(1, H, device="cuda")
+        save = torch.empty(-(-T // 8), 1, H, device="cuda")
+        B.approx_lstm_linear_run(p.view(T, 1, 4 * H), h, c0=c0, c_out=c, c_save=save)
+        assert torch.equal(c, c0)
+        want = torch.tanh(c0.double())
+        assert ((h.double() - want).abs() <= 10 * 2.0 ** -24 + HALF[dtype] * want.abs()).all()
+        dp, dc0 = torch.full_like(p, float("nan")).view(T, 1, 4 * H), torch.full_like(c0, float("nan"))
+        dc = torch.ones_like(c0)
+        B.approx_lstm_linear_backward(p.view(T, 1, 4 * H), torch.zeros_like(h), save, dp, dc_out=dc, dc0=dc0)
+        assert torch.equal(dc0, dc) and not dp.any()
+        p[:, :, 1] = -v          # f closed, i open, g at -1: the state is -1
+        p[:, :, 0] = v
+        p[:, :, 2] = -v
+        B.approx_lstm_linear_run(p.view(T, 1, 4 * H), h, c0=c0, c_out=c)
+        assert (c == -1).all()
+
+
+@pytest.mark.parametrize("T,Bn,H", [(200, 3, 64), (3000, 1, 32)])
+def test_a_nan_stays_in_its_sequence_and_unit(T, Bn, H):
+    say("nan", T, Bn, H)
+    k = Case(T, Bn, H, seed=3)
+    clean, dirty = k.out(), k.out()
+    k.run(clean)
+    at = T // 2
+    k.p[at, 0, H + 5] = float("nan")
+    k.run(dirty)
+    same = dirty["h"] == clean["h"]
+    hurt = torch.zeros_like(same)
+    hurt[at:, 0, 5] = True
+    assert torch.equal(same, ~hurt) and torch.isnan(dirty["h"][at:, 0, 5]).all()
+
+
+@pytest.mark.parametrize("T,Bn,H", [(1, 4, 64), (200, 2, 96), (5000, 1, 64)])
+def test_captured_and_replayed(T, Bn, H):
+    """Two graphs with a workspace each, replayed several times with eager work
+    between: always the eager bits."""
+    say("graph", T, Bn, H)
+    k = Case(T, Bn, H, BF16)
+    o, eager = k.out(), k.out()
+    k.run(eager)
+    k.back(eager)
+    torch.cuda.synchronize()
+    n = max(1, B.approx_lstm_linear_workspace(T, Bn, H), B.approx_lstm_linear_workspace(T, Bn, H, 2))
+    ws = [torch.empty(n + 16, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    graphs = []
+    for w in ws:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            k.run(o, workspace=w)
+            k.back(o, workspace=w)
+        graphs.append(g)
+    for r in range(4):
+        for t in o.values():
+            t.fill_(float("nan"))
+        for w in ws:
+            w.fill_(17 * r)
+        graphs[r % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[m], eager[m]) for m in o), r
+        other = k.out()
+        k.run(other)
+        torch.cuda.synchronize()
+        assert torch.equal(other["h"], eager["h"])
+
+
+def test_two_streams_at_once():
+    ks = [Case(3000, 1, 64, seed=s) for s in range(2)]
+    want = [k.out() for k in ks]
+    for k, o in zip(ks, want):
+        k.run(o)
+        k.back(o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ks]
+    got = [k.out() for k in ks]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k, o, s in zip(ks, got, streams):
+            k.run(o, stream=s)
+            k.back(o, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(got, want):
+        assert all(torch.equal(o[n], w[n]) for n in o)
+
+
+def test_refusals_on_the_device():
+    k = Case(300, 2, 64)
+    o = k.out()
+    n = B.approx_lstm_linear_workspace(300, 2, 64, 2)
+    assert n
+    for ws in (torch.empty(n - 1, dtype=torch.uint8, device="cuda"),
+               torch.empty(n + 16, dtype=torch.uint8, device="cuda")[1:]):
+        with pytest.raises(B.ApproxLstmError):
+            k.back(o, workspace=ws)
+    for bad in (dict(bias=k.bias[:-1]), dict(c0=k.c0.double()), dict(lengths=torch.zeros(1, device="cuda")),
+                dict(c_out=torch.empty(2, 128, device="cuda")[:, ::2]), dict(c_save=o["save"][1:])):
+        with pytest.raises((TypeError, ValueError)):
+            B.approx_lstm_linear_run(k.p, o["h"], **bad)
+    with pytest.raises(TypeError):
+        B.approx_lstm_linear_run(k.p.transpose(0, 1), o["h"])
+    with pytest.raises(TypeError):
+        B.approx_lstm_linear_run(k.p.half(), o["h"])
+    assert all(torch.isnan(t).all() for t in o.values())
