@@ -1715,6 +1715,7 @@ approx_lstm_status check_linear(alstm::LinearArgs& a, int dtype, int backward, c
   const size_t el = dtype ? 2 : 4;
   if ((uint64_t)a.B * a.H * 4 * el >= (1ull << 31))
     return fail(APPROX_LSTM_ERR_UNSUPPORTED, "B = %d, H = %d: a timestep of 2 GiB or more", a.B, a.H);
+  if (a.T > INT32_MAX - 1024) return fail(APPROX_LSTM_ERR_UNSUPPORTED, "T = %d exceeds 2^31 - 1025", a.T);
   for (const void* p : {a.p, (const void*)a.h, a.dh, (const void*)a.dp})
     if (!aligned(p, el)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "p, h or a gradient not aligned to its elements");
   for (const void* p : {(const void*)a.bias, (const void*)a.lengths, (const void*)a.c0, (const void*)a.c_out,
@@ -1784,6 +1785,8 @@ approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H,
   g_last_error.clear();
   if (!bytes) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null bytes");
   if (T < 0 || B < 1 || H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 0, B >= 1 and H >= 1");
+  if (T > INT32_MAX - 1024 || (uint64_t)B * H >= (1ull << 29))
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "sizes beyond those of a run");
   if (backward < 0 || backward > 2) return fail(APPROX_LSTM_ERR_INVALID_ARG, "backward = %d not in 0..2", backward);
   int num_cu = 0;
   approx_lstm_status st = current_cus(&num_cu);

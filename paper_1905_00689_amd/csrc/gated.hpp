@@ -33,6 +33,14 @@ struct LinearArgs {
   float* dpart;           // [rows][4H]: sums of dp, one row per sequence (and stretch of time)
 };
 
+// Where the chunks of time of a column (64 pairs of units) hand over (linear.hip).
+struct LinearScan {
+  int cols, chunks, lanes;       // columns, chunks of time, pairs of units
+  unsigned long long* maps;      // [chunks][lanes][2]: (A, B) of a unit
+  unsigned* states;              // [groups][lanes][2]
+  unsigned* tickets;             // [cols], 64 bytes apart
+};
+
 // Bytes of workspace of a run (backward 0), a backward pass (1) or one with the
 // bias gradient (2).
 size_t linear_workspace(int T, int B, int H, int num_cu, int backward);

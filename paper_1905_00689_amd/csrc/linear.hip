@@ -3,128 +3,668 @@
 //
 //   c_t = sigmoid(f_t) c_{t-1} + sigmoid(i_t) tanh(g_t),   h_t = sigmoid(o_t) tanh(c_t),
 //
-// and its gradients.  Every (sequence, unit) is a recurrence of its own.
+// and its gradients.  Every (sequence, unit) is a recurrence of its own, linear in
+// its state: a stretch of time maps c to A c + B with A = prod f and B the state
+// it leaves from 0, and two stretches compose as (A2 A1, A2 B1 + B2).  So time is
+// split twice: a wave takes 8 timesteps of 128 units in registers, a workgroup
+// eight such waves (a chunk of 64), whose maps meet in LDS.  Each wave then runs
+// its 8 steps from its own first state, so p is read once and nothing but maps is
+// exchanged.  Every composition has a fixed order: same bits whatever runs beside.
 #include <algorithm>
 
 #include "device_common.hpp"
 #include "gated.hpp"
 
+// every fused multiply-add is written out: same bits from every instance
+#pragma clang fp contract(off)
+
 namespace alstm {
 
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kSteps = kLinearSave;            // timesteps of a wave
+constexpr int kScanWaves = 8;
+constexpr int kScanThreads = 64 * kScanWaves;
+constexpr int kChunk = kSteps * kScanWaves;    // timesteps of a workgroup at once
+constexpr int kGroup = 32;                     // chunks between two handed-on states
+constexpr int kPolls = kGroup / kScanWaves;    // maps a wave collects
+constexpr int kTicketStride = 16;              // words between two columns' tickets (64 bytes)
 constexpr int kWalkThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f;
 
+// Two neighbouring units of a row.  VEC: both there (H even) and the pair aligned;
+// else read one by one, `two` false where the second is past the row (it then
+// reads the first again).
 template <class T>
-__device__ __forceinline__ float to_f32(T v) { return (float)v; }
+struct Pair;
+template <>
+struct Pair<float> {
+  typedef f32x2 Raw;
+  static __device__ __forceinline__ f32x2 get(Raw r) { return r; }
+  static __device__ __forceinline__ Raw put(f32x2 v) { return v; }
+  static __device__ __forceinline__ Raw join(const float* p, bool two) { return Raw{p[0], p[two ? 1 : 0]}; }
+  static __device__ __forceinline__ void split(float* p, Raw r, bool two) {
+    p[0] = r[0];
+    if (two) p[1] = r[1];
+  }
+};
+template <>
+struct Pair<__bf16> {
+  typedef unsigned Raw;
+  static __device__ __forceinline__ f32x2 get(Raw r) {
+    return f32x2{__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u)};
+  }
+  static __device__ __forceinline__ Raw put(f32x2 v) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));   // to the nearest, ties to even
+  }
+  static __device__ __forceinline__ Raw join(const __bf16* p, bool two) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    return (unsigned)q[0] | ((unsigned)q[two ? 1 : 0] << 16);
+  }
+  static __device__ __forceinline__ void split(__bf16* p, Raw r, bool two) {
+    uint16_t* q = reinterpret_cast<uint16_t*>(p);
+    q[0] = (uint16_t)r;
+    if (two) q[1] = (uint16_t)(r >> 16);
+  }
+};
 
-__device__ __forceinline__ float sig(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
-__device__ __forceinline__ float tnh(float x) { return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __expf(2.0f * x)), 1.0f); }
+template <class T, bool VEC>
+__device__ __forceinline__ typename Pair<T>::Raw load_pair(const char* row, unsigned off, bool two) {
+  const T* p = reinterpret_cast<const T*>(row + off);
+  if constexpr (VEC) return *reinterpret_cast<const typename Pair<T>::Raw*>(p);
+  else return Pair<T>::join(p, two);
+}
 
-template <class T>
+template <class T, bool VEC>
+__device__ __forceinline__ void store_pair(char* row, unsigned off, f32x2 v, bool two) {
+  T* p = reinterpret_cast<T*>(row + off);
+  const auto r = Pair<T>::put(v);
+  if constexpr (VEC) *reinterpret_cast<typename Pair<T>::Raw*>(p) = r;
+  else Pair<T>::split(p, r, two);
+}
+
+template <bool VEC>
+__device__ __forceinline__ f32x2 load_state(const float* p, bool two) {
+  return load_pair<float, VEC>(reinterpret_cast<const char*>(p), 0, two);
+}
+template <bool VEC>
+__device__ __forceinline__ void store_state(float* p, f32x2 v, bool two) {
+  store_pair<float, VEC>(reinterpret_cast<char*>(p), 0, v, two);
+}
+
+// What a lane works on: units r, r + 1 of sequence b.
+struct Lane {
+  int b, r, len;          // len: timesteps of the sequence
+  bool live, two;         // live: there is such a sequence
+  unsigned at;            // its place in a row of states [B][H] (elements)
+};
+
+__device__ __forceinline__ Lane lane_of(const LinearArgs& a, int idx) {
+  Lane l;
+  const int pairs = (a.H + 1) / 2;
+  l.live = idx < a.B * pairs;
+  if (!l.live) idx = 0;
+  l.b = idx / pairs;
+  l.r = 2 * (idx - l.b * pairs);
+  l.two = l.r + 1 < a.H;
+  l.at = (unsigned)l.b * (unsigned)a.H + (unsigned)l.r;
+  l.len = a.lengths ? min(max(a.lengths[l.b], 0), a.T) : a.T;
+  return l;
+}
+
+// Gates with the bias inside the exponential's argument: sigmoid(x + b) = 1 / (1 +
+// 2^(k x + k b)), k = -log2 e, and tanh(x + b) = 1 - 2 / (1 + 2^(-2 k (x + b))).
+// Both reach their ends exactly (2^x is 0 or infinity there).
+struct GateBias {
+  f32x2 i, f, g, o;
+};
+
+template <bool VEC>
+__device__ __forceinline__ GateBias gate_bias(const LinearArgs& a, const Lane& l) {
+  GateBias b{};
+  if (a.bias) {
+    // (the bias need be aligned to its elements only)
+    auto at = [&](int q) {
+      const float* p = a.bias + (size_t)q * a.H + l.r;
+      return f32x2{p[0], p[l.two ? 1 : 0]};
+    };
+    b.i = at(0) * -kLog2e, b.f = at(1) * -kLog2e, b.g = at(2) * (2.0f * kLog2e), b.o = at(3) * -kLog2e;
+  }
+  return b;
+}
+
+__device__ __forceinline__ float gate_sig(float x, float b) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, -kLog2e, b)));
+}
+// The forget gate: over a memory of 1 / (1 - f) steps an error of the same sign in
+// each adds up, and the reciprocal's is (0.1 of half a step on average at f near 1;
+// 0.006 after one Newton step).  fminf keeps 0 x infinity out where the gate is shut.
+__device__ __forceinline__ float gate_forget(float x, float b) {
+  const float d = 1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, -kLog2e, b)), r = __builtin_amdgcn_rcpf(d);
+  return __builtin_fmaf(fminf(__builtin_fmaf(-r, d, 1.0f), 1e-6f), r, r);
+}
+__device__ __forceinline__ float gate_tanh(float x, float b) {
+  return __builtin_fmaf(
+      -2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, 2.0f * kLog2e, b))), 1.0f);
+}
+
+// Few timesteps: a lane walks its two units through all of them, the loads of
+// kAhead timesteps at once.
+template <class T, bool VEC>
 __global__ void __launch_bounds__(kWalkThreads) linear_walk_kernel(LinearArgs a) {
-  const size_t i = (size_t)blockIdx.x * kWalkThreads + threadIdx.x, BH = (size_t)a.B * a.H;
-  if (i >= BH) return;
-  const int b = (int)(i / a.H), r = (int)(i % a.H), H = a.H;
-  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-  float bi = 0.f, bf = 0.f, bg = 0.f, bo = 0.f;
-  if (a.bias) bi = a.bias[r], bf = a.bias[H + r], bg = a.bias[2 * H + r], bo = a.bias[3 * H + r];
-  float c = a.c0 ? a.c0[i] : 0.f;
-  for (int t = 0; t < a.T; ++t) {
-    if (a.c_save && t % kLinearSave == 0) a.c_save[(size_t)(t / kLinearSave) * BH + i] = c;
-    float h = 0.f;
-    if (t < len) {
-      const T* p = (const T*)a.p + ((size_t)t * a.B + b) * 4 * H + r;
-      c = __builtin_fmaf(sig((float)p[H] + bf), c, sig((float)p[0] + bi) * tnh((float)p[2 * H] + bg));
-      h = sig((float)p[3 * H] + bo) * tnh(c);
-    }
-    ((T*)a.h)[(size_t)t * BH + i] = (T)h;
-  }
-  if (a.c_out) a.c_out[i] = c;
-}
-
-template <class T>
-__global__ void __launch_bounds__(kWalkThreads) linear_back_kernel(LinearArgs a) {
-  const size_t i = (size_t)blockIdx.x * kWalkThreads + threadIdx.x, BH = (size_t)a.B * a.H;
-  if (i >= BH) return;
-  const int b = (int)(i / a.H), r = (int)(i % a.H), H = a.H;
-  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-  float bi = 0.f, bf = 0.f, bg = 0.f, bo = 0.f;
-  if (a.bias) bi = a.bias[r], bf = a.bias[H + r], bg = a.bias[2 * H + r], bo = a.bias[3 * H + r];
-  float e = a.dc_out ? a.dc_out[i] : 0.f;
-  float si = 0.f, sf = 0.f, sg = 0.f, so = 0.f;
-  for (int t0 = (a.T - 1) / kLinearSave * kLinearSave; t0 >= 0; t0 -= kLinearSave) {
-    float cs[kLinearSave + 1];
-    cs[0] = a.c_save[(size_t)(t0 / kLinearSave) * BH + i];
+  constexpr int kAhead = 4;
+  const Lane l = lane_of(a, blockIdx.x * kWalkThreads + threadIdx.x);
+  if (!l.live) return;
+  const GateBias bias = gate_bias<VEC>(a, l);
+  const size_t BH = (size_t)a.B * a.H;
+  const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T);
+  f32x2 c = a.c0 ? load_state<VEC>(a.c0 + l.at, l.two) : f32x2{0.f, 0.f};
+  for (int t0 = 0; t0 < a.T; t0 += kAhead) {
+    typename Pair<T>::Raw raw[kAhead][4];
 #pragma unroll
-    for (int k = 0; k < kLinearSave; ++k) {
-      cs[k + 1] = cs[k];
-      if (t0 + k < len) {
-        const T* p = (const T*)a.p + ((size_t)(t0 + k) * a.B + b) * 4 * H + r;
-        cs[k + 1] = __builtin_fmaf(sig((float)p[H] + bf), cs[k], sig((float)p[0] + bi) * tnh((float)p[2 * H] + bg));
-      }
+    for (int s = 0; s < kAhead; ++s) {
+      const char* row = (const char*)a.p + (size_t)min(t0 + s, a.T - 1) * (4 * BH * sizeof(T));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) raw[s][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
     }
 #pragma unroll
-    for (int k = kLinearSave - 1; k >= 0; --k) {
-      const int t = t0 + k;
-      if (t >= a.T) continue;
-      float di = 0.f, df = 0.f, dg = 0.f, dO = 0.f;
-      if (t < len) {
-        const T* p = (const T*)a.p + ((size_t)t * a.B + b) * 4 * H + r;
-        const float vi = sig((float)p[0] + bi), vf = sig((float)p[H] + bf), vg = tnh((float)p[2 * H] + bg),
-                    vo = sig((float)p[3 * H] + bo), tc = tnh(cs[k + 1]);
-        const float dh = (float)((const T*)a.dh)[(size_t)t * BH + i];
-        const float d = __builtin_fmaf(dh * vo, 1.f - tc * tc, e);
-        di = d * vg * (vi * (1.f - vi));
-        df = d * cs[k] * (vf * (1.f - vf));
-        dg = d * vi * (1.f - vg * vg);
-        dO = dh * tc * (vo * (1.f - vo));
-        e = vf * d;
+    for (int s = 0; s < kAhead; ++s) {
+      const int t = t0 + s;
+      if (t >= a.T) break;
+      if (s % kSteps == 0 && t % kSteps == 0 && a.c_save)
+        store_state<VEC>(a.c_save + (size_t)(t / kSteps) * BH + l.at, c, l.two);
+      const f32x2 yi = Pair<T>::get(raw[s][0]), yf = Pair<T>::get(raw[s][1]), yg = Pair<T>::get(raw[s][2]),
+                  yo = Pair<T>::get(raw[s][3]);
+      f32x2 h{0.f, 0.f};
+      if (t < l.len) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          c[k] = __builtin_fmaf(gate_forget(yf[k], bias.f[k]), c[k], gate_sig(yi[k], bias.i[k]) * gate_tanh(yg[k], bias.g[k]));
+          h[k] = gate_sig(yo[k], bias.o[k]) * gate_tanh(c[k], 0.f);
+        }
       }
-      T* dp = (T*)a.dp + ((size_t)t * a.B + b) * 4 * H + r;
-      dp[0] = (T)di, dp[H] = (T)df, dp[2 * H] = (T)dg, dp[3 * H] = (T)dO;
-      si += di, sf += df, sg += dg, so += dO;
+      store_pair<T, VEC>((char*)a.h + (size_t)t * (BH * sizeof(T)), l.at * sizeof(T), h, l.two);
     }
   }
-  if (a.dc0) a.dc0[i] = e;
-  if (a.dbias) {
-    float* s = a.dpart + (size_t)b * 4 * H + r;
-    s[0] = si, s[H] = sf, s[2 * H] = sg, s[3 * H] = so;
+  if (a.c_out) store_state<VEC>(a.c_out + l.at, c, l.two);
+}
+
+// A map c -> A c + B of two units, {A0, B0, A1, B1}.
+__device__ __forceinline__ f32x4 then(const f32x4& first, const f32x4& second) {
+  return f32x4{second[0] * first[0], __builtin_fmaf(second[0], first[1], second[1]), second[2] * first[2],
+               __builtin_fmaf(second[2], first[3], second[3])};
+}
+__device__ __forceinline__ f32x2 apply(const f32x4& m, const f32x2& c) {
+  return f32x2{__builtin_fmaf(m[0], c[0], m[1]), __builtin_fmaf(m[2], c[1], m[3])};
+}
+constexpr f32x4 kIdentity{1.f, 0.f, 1.f, 0.f};
+
+// Hand-over between chunks of a column, when there are too few columns to fill the
+// device and so its chunks run side by side.  A word is empty (all ones, as the
+// kernel before cleared it) until its value is there; a value with the bits of an
+// empty word is written as another NaN.  A chunk publishes its map as soon as it
+// has it, collects the maps of the chunks before it in its group of kGroup, and
+// waits for the one state that the group before handed on; the last chunk of a
+// group hands on its own.  So a hop of the serial chain passes kGroup chunks.
+//
+// Which chunk a workgroup takes is the ticket of its column: in the order in which
+// workgroups start, so the chunks that anyone waits for have workgroups that run.
+__device__ __forceinline__ unsigned filled(float v) {
+  const unsigned w = __float_as_uint(v);
+  return w == kEmpty ? 0x7FC00000u : w;
+}
+
+__device__ __forceinline__ void publish_map(unsigned long long* w, const f32x4& m) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    __hip_atomic_store(w + k, ((unsigned long long)filled(m[2 * k]) << 32) | __float_as_uint(m[2 * k + 1]), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void publish_state(unsigned* w, const f32x2& c) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    __hip_atomic_store(w + k, filled(c[k]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// the state of a word pair; NaN past the spin limit
+__device__ __forceinline__ f32x2 await_state(const unsigned* w) {
+  unsigned v[2], spins = 0;
+  while (true) {
+    v[0] = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v[1] = __hip_atomic_load(w + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((v[0] != kEmpty && v[1] != kEmpty) || ++spins >= kSpinLimit) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  return f32x2{__uint_as_float(v[0]), __uint_as_float(v[1])};   // (an empty word is a NaN)
+}
+
+// the composition of n (1 .. kPolls) maps, `stride` words apart; NaN past the limit
+__device__ __forceinline__ f32x4 await_maps(const unsigned long long* w, size_t stride, int n) {
+  unsigned long long v[kPolls][2];
+  unsigned spins = 0;
+  while (true) {
+    bool all = true;
+#pragma unroll
+    for (int j = 0; j < kPolls; ++j)
+      if (j < n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          v[j][k] = __hip_atomic_load(w + j * stride + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int j = 0; j < kPolls; ++j)
+      if (j < n) all = all && (unsigned)(v[j][0] >> 32) != kEmpty && (unsigned)(v[j][1] >> 32) != kEmpty;
+    if (all || ++spins >= kSpinLimit) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  f32x4 m = kIdentity;
+#pragma unroll
+  for (int j = 0; j < kPolls; ++j)
+    if (j < n)
+      m = then(m, f32x4{__uint_as_float((unsigned)(v[j][0] >> 32)), __uint_as_float((unsigned)v[j][0]),
+                        __uint_as_float((unsigned)(v[j][1] >> 32)), __uint_as_float((unsigned)v[j][1])});
+  return m;
+}
+
+struct ScanLds {
+  f32x4 wave[2][kScanWaves][64];   // maps of the waves (of even and odd rounds)
+  f32x4 before[kScanWaves][64];    // maps that the waves collected
+  f32x2 entry[64];                 // the state that the group begins with
+  int ticket;
+};
+
+// The state that this chunk (the `order`-th of its column) begins with, where
+// chunks hand over; `wave_order` is the wave's place in time.  The waves' maps are
+// in lds.wave[0], by place.  `first` is where the column's first state stands: it is
+// read by the first chunk alone, which hands it on too, since the last chunk's
+// state may be written to the same place.
+template <class Load>
+__device__ __forceinline__ f32x2 hand_over(ScanLds& lds, const LinearScan& s, int order, int wave_order, int lane,
+                                           size_t idx, bool live, Load first) {
+  const int g = order / kGroup, r = order - g * kGroup;
+  const bool last = order + 1 >= s.chunks;
+  const size_t stride = 2 * (size_t)s.lanes;
+  if (wave_order == kScanWaves - 1 && !last && r != kGroup - 1) {
+    f32x4 m = lds.wave[0][0][lane];
+#pragma unroll
+    for (int w = 1; w < kScanWaves; ++w) m = then(m, lds.wave[0][w][lane]);
+    if (live) publish_map(s.maps + order * stride + 2 * idx, m);
+  }
+  const int have = r - kPolls * wave_order;   // maps before this chunk that are left to this wave
+  if (have > 0)
+    lds.before[wave_order][lane] =
+        live ? await_maps(s.maps + (size_t)(g * kGroup + kPolls * wave_order) * stride + 2 * idx, stride, min(have, kPolls))
+             : kIdentity;
+  lds_barrier();
+  if (wave_order == 0) {
+    f32x4 m = kIdentity;
+    const bool hands_on = r == kGroup - 1 && !last;
+    if (hands_on) {   // composed before the state comes, one step when it is there
+#pragma unroll
+      for (int w = 0; w < kScanWaves; ++w)
+        if (kPolls * w < r) m = then(m, lds.before[w][lane]);
+#pragma unroll
+      for (int w = 0; w < kScanWaves; ++w) m = then(m, lds.wave[0][w][lane]);
+    }
+    f32x2 c{0.f, 0.f};
+    if (order == 0) {
+      c = first();
+      if (live && !last) publish_state(s.states + 2 * idx, c);
+    } else if (live) {
+      c = await_state(s.states + g * stride + 2 * idx);
+    }
+    if (hands_on && live) publish_state(s.states + (g + 1) * stride + 2 * idx, apply(m, c));
+    lds.entry[lane] = c;
+  }
+  lds_barrier();
+  f32x2 c = lds.entry[lane];
+#pragma unroll
+  for (int w = 0; w < kScanWaves; ++w)
+    if (kPolls * w < r) c = apply(lds.before[w][lane], c);
+  return c;
+}
+
+// LOOK: a workgroup takes one chunk and chunks hand over; else it takes its
+// column's chunks one after another and keeps the state.
+template <class T, bool VEC, bool LOOK>
+__global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs a, LinearScan s) {
+  __shared__ ScanLds lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int col = blockIdx.x, chunk = 0;
+  if constexpr (LOOK) {
+    col = blockIdx.x % s.cols;
+    if (threadIdx.x == 0)
+      lds.ticket = (int)__hip_atomic_fetch_add(s.tickets + (size_t)col * kTicketStride, 1u, __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    lds_barrier();
+    chunk = __builtin_amdgcn_readfirstlane(lds.ticket);
+  }
+  const int idx = col * 64 + lane;
+  const Lane l = lane_of(a, idx);
+  const GateBias bias = gate_bias<VEC>(a, l);
+  const size_t BH = (size_t)a.B * a.H;
+  const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T), ha = l.at * sizeof(T);
+  auto first = [&] { return a.c0 ? load_state<VEC>(a.c0 + l.at, l.two) : f32x2{0.f, 0.f}; };
+  if (!LOOK && wave == 0) lds.entry[lane] = first();   // (one wave reads it: c_out may be c0)
+  f32x2 carry{0.f, 0.f};
+  for (; chunk < s.chunks; ++chunk) {
+    const int t0 = chunk * kChunk + wave * kSteps;
+    typename Pair<T>::Raw raw[kSteps][4];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const char* row = (const char*)a.p + (size_t)min(t0 + k, a.T - 1) * (4 * BH * sizeof(T));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
+    }
+    f32x2 f[kSteps], u[kSteps], o[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]),
+                  yo = Pair<T>::get(raw[k][3]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f[k][j] = gate_forget(yf[j], bias.f[j]);
+        u[k][j] = gate_sig(yi[j], bias.i[j]) * gate_tanh(yg[j], bias.g[j]);
+        o[k][j] = gate_sig(yo[j], bias.o[j]);
+      }
+    }
+    const int n = min(l.len - t0, kSteps);   // timesteps here that the sequence has
+    if (a.lengths || t0 + kSteps > a.T) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+        if (k >= n) f[k] = f32x2{1.f, 1.f}, u[k] = f32x2{0.f, 0.f};
+    }
+    f32x4 m{f[0][0], u[0][0], f[0][1], u[0][1]};
+#pragma unroll
+    for (int k = 1; k < kSteps; ++k) m = then(m, f32x4{f[k][0], u[k][0], f[k][1], u[k][1]});
+    const int half = LOOK ? 0 : chunk & 1;
+    lds.wave[half][wave][lane] = m;
+    lds_barrier();
+    f32x2 c = !LOOK && chunk == 0 ? lds.entry[lane] : carry;
+    if constexpr (LOOK) c = hand_over(lds, s, chunk, wave, lane, idx, l.live, first);
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w) {
+      if (w == wave) carry = c;
+      if (LOOK && w == wave) break;
+      c = apply(lds.wave[half][w][lane], c);
+    }
+    f32x2 next = c;
+    c = carry;          // the wave's first state
+    carry = next;       // the chunk's last one
+    if (l.live) {
+      if (a.c_save && t0 < a.T) store_state<VEC>(a.c_save + (size_t)(t0 / kSteps) * BH + l.at, c, l.two);
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        f32x2 h;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          c[j] = __builtin_fmaf(f[k][j], c[j], u[k][j]);
+          h[j] = o[k][j] * gate_tanh(c[j], 0.f);
+          if (k >= n) h[j] = 0.f;
+        }
+        if (t0 + k < a.T) store_pair<T, VEC>((char*)a.h + (size_t)(t0 + k) * (BH * sizeof(T)), ha, h, l.two);
+      }
+      if (a.c_out && chunk == s.chunks - 1 && wave == kScanWaves - 1) store_state<VEC>(a.c_out + l.at, c, l.two);
+    }
+    if constexpr (LOOK) break;
   }
 }
 
-// dbias[k] = the sum of the rows of dpart, in order
-__global__ void __launch_bounds__(64) linear_dbias_kernel(const float* dpart, int rows, int n, float* dbias) {
-  const int k = blockIdx.x * 64 + threadIdx.x;
-  if (k >= n) return;
-  float s = 0.f;
-  for (int r = 0; r < rows; ++r) s += dpart[(size_t)r * n + k];
-  dbias[k] = s;
+// The backward pass, the same from the end: with e the gradient that c_t gets from
+// later timesteps and w_t = dh_t o_t (1 - tanh(c_t)^2),
+//
+//   d_t = w_t + e_t,  e_{t-1} = f_t d_t,  dp = d g i (1-i), d c_{t-1} f (1-f), d i (1-g^2), dh tanh(c) o (1-o).
+//
+// A wave runs its 8 steps forward from the saved state, so c is neither stored nor
+// read but every 8 timesteps, and keeps f, w and the three factors of d; its map is
+// e -> A e + B again.  The sums of dp over its timesteps leave through dpart.
+template <class T, bool VEC, bool LOOK>
+__global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs a, LinearScan s) {
+  __shared__ ScanLds lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int col = blockIdx.x, order = 0;
+  if constexpr (LOOK) {
+    col = blockIdx.x % s.cols;
+    if (threadIdx.x == 0)
+      lds.ticket = (int)__hip_atomic_fetch_add(s.tickets + (size_t)col * kTicketStride, 1u, __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    lds_barrier();
+    order = __builtin_amdgcn_readfirstlane(lds.ticket);
+  }
+  const int idx = col * 64 + lane;
+  const Lane l = lane_of(a, idx);
+  const GateBias bias = gate_bias<VEC>(a, l);
+  const size_t BH = (size_t)a.B * a.H;
+  const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T), ha = l.at * sizeof(T);
+  const int place = kScanWaves - 1 - wave;   // the wave's place in the order of the pass
+  auto first = [&] { return a.dc_out ? load_state<VEC>(a.dc_out + l.at, l.two) : f32x2{0.f, 0.f}; };
+  if (!LOOK && place == 0) lds.entry[lane] = first();   // (one wave reads it: dc0 may be dc_out)
+  f32x2 carry{0.f, 0.f};
+  f32x2 si{0.f, 0.f}, sf = si, sg = si, so = si;
+  for (; order < s.chunks; ++order) {
+    const int chunk = s.chunks - 1 - order, t0 = chunk * kChunk + wave * kSteps;
+    typename Pair<T>::Raw raw[kSteps][4], rdh[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const size_t t = (size_t)min(t0 + k, a.T - 1);
+      const char* row = (const char*)a.p + t * (4 * BH * sizeof(T));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
+      rdh[k] = load_pair<T, VEC>((const char*)a.dh + t * (BH * sizeof(T)), ha, l.two);
+    }
+    f32x2 c = load_state<VEC>(a.c_save + (size_t)(min(t0, a.T - 1) / kSteps) * BH + l.at, l.two);
+    const int n = min(l.len - t0, kSteps);
+    f32x2 f[kSteps], w[kSteps], ki[kSteps], kf[kSteps], kg[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]),
+                  yo = Pair<T>::get(raw[k][3]), dh = Pair<T>::get(rdh[k]);
+      f32x2 dO;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float vf = gate_forget(yf[j], bias.f[j]), vi = gate_sig(yi[j], bias.i[j]), vg = gate_tanh(yg[j], bias.g[j]),
+                    vo = gate_sig(yo[j], bias.o[j]);
+        kf[k][j] = c[j] * __builtin_fmaf(-vf, vf, vf);
+        ki[k][j] = vg * __builtin_fmaf(-vi, vi, vi);
+        kg[k][j] = vi * __builtin_fmaf(-vg, vg, 1.f);
+        const float cn = __builtin_fmaf(vf, c[j], vi * vg), tc = gate_tanh(cn, 0.f), dho = dh[j] * vo;
+        f[k][j] = vf;
+        w[k][j] = dho * __builtin_fmaf(-tc, tc, 1.f);
+        dO[j] = dho * tc * (1.f - vo);
+        if (k >= n) f[k][j] = 1.f, w[k][j] = kf[k][j] = ki[k][j] = kg[k][j] = dO[j] = 0.f;
+        else c[j] = cn;
+        so[j] += dO[j];
+      }
+      if (l.live && t0 + k < a.T)
+        store_pair<T, VEC>((char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T)), ga + 3 * gs, dO, l.two);
+    }
+    f32x4 m = kIdentity;
+#pragma unroll
+    for (int k = kSteps - 1; k >= 0; --k)
+      m = then(m, f32x4{f[k][0], f[k][0] * w[k][0], f[k][1], f[k][1] * w[k][1]});
+    const int half = LOOK ? 0 : order & 1;
+    lds.wave[half][place][lane] = m;
+    lds_barrier();
+    f32x2 e = !LOOK && order == 0 ? lds.entry[lane] : carry;
+    if constexpr (LOOK) e = hand_over(lds, s, order, place, lane, idx, l.live, first);
+#pragma unroll
+    for (int v = 0; v < kScanWaves; ++v) {
+      if (v == place) carry = e;
+      if (LOOK && v == place) break;
+      e = apply(lds.wave[half][v][lane], e);
+    }
+    f32x2 next = e;
+    e = carry;
+    carry = next;
+#pragma unroll
+    for (int k = kSteps - 1; k >= 0; --k) {
+      f32x2 di, df, dg;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float d = w[k][j] + e[j];
+        di[j] = d * ki[k][j], df[j] = d * kf[k][j], dg[j] = d * kg[k][j];
+        e[j] = f[k][j] * d;
+        si[j] += di[j], sf[j] += df[j], sg[j] += dg[j];
+      }
+      if (l.live && t0 + k < a.T) {
+        char* row = (char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T));
+        store_pair<T, VEC>(row, ga, di, l.two);
+        store_pair<T, VEC>(row, ga + gs, df, l.two);
+        store_pair<T, VEC>(row, ga + 2 * gs, dg, l.two);
+      }
+    }
+    if (a.dc0 && l.live && chunk == 0 && wave == 0) store_state<VEC>(a.dc0 + l.at, e, l.two);
+    if constexpr (LOOK) break;
+  }
+  if (!a.dbias) return;
+  // sums of the waves, in order (lds.wave is 2 x kScanWaves rows of 64)
+  lds_barrier();
+  lds.wave[0][wave][lane] = f32x4{si[0], si[1], sf[0], sf[1]};
+  lds.wave[1][wave][lane] = f32x4{sg[0], sg[1], so[0], so[1]};
+  lds_barrier();
+  if (wave < 2 && l.live) {
+    f32x4 t = lds.wave[wave][0][lane];
+#pragma unroll
+    for (int v = 1; v < kScanWaves; ++v) t += lds.wave[wave][v][lane];
+    float* row = a.dpart + ((size_t)(LOOK ? order : 0) * a.B + l.b) * (4 * (size_t)a.H) + (size_t)2 * wave * a.H + l.r;
+    row[0] = t[0], row[a.H] = t[2];
+    if (l.two) row[1] = t[1], row[a.H + 1] = t[3];
+  }
+}
+
+// dbias[k] = the sum of the rows of dpart: 32 columns and 32 runs of rows a
+// workgroup, the runs summed in order.
+__global__ void __launch_bounds__(1024) linear_dbias_kernel(const float* dpart, int rows, int n, float* dbias) {
+  __shared__ float part[32][33];
+  const int c = threadIdx.x & 31, q = threadIdx.x >> 5, k = blockIdx.x * 32 + c;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (k < n) {
+    int r = q;
+    for (; r + 96 < rows; r += 128)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += dpart[(size_t)(r + 32 * j) * n + k];
+    for (; r < rows; r += 32) s[0] += dpart[(size_t)r * n + k];
+  }
+  part[q][c] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (q != 0 || k >= n) return;
+  float t = part[0][c];
+  for (int j = 1; j < 32; ++j) t += part[j][c];
+  dbias[k] = t;
+}
+
+// Empties the hand-over words and the tickets.
+__global__ void __launch_bounds__(256) linear_clear_kernel(u32x4* words, size_t n, u32x4* tickets, size_t nt) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n + nt; i += (size_t)gridDim.x * 256) {
+    if (i < n) words[i] = u32x4{kEmpty, kEmpty, kEmpty, kEmpty};
+    else tickets[i - n] = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+
+struct Plan {
+  LinearScan s;
+  bool walk, look;
+  size_t lanes;          // pairs of units
+  size_t maps, states, tickets, dpart;   // bytes
+  int rows;              // of dpart
+};
+
+Plan plan_of(int T, int B, int H, int num_cu, int backward) {
+  Plan p{};
+  const int pairs = (H + 1) / 2;
+  p.lanes = (size_t)B * pairs;
+  p.s.lanes = (int)p.lanes;
+  p.s.cols = (int)((p.lanes + 63) / 64);
+  p.s.chunks = std::max(1, (T + kChunk - 1) / kChunk);
+  p.walk = !backward && T <= 16;
+  // (a grid has fewer than 2^32 threads)
+  p.look = !p.walk && p.s.chunks > 1 && p.s.cols < 2 * num_cu && (size_t)p.s.cols * p.s.chunks <= (1u << 22);
+  if (p.look) {
+    const size_t groups = (size_t)(p.s.chunks + kGroup - 1) / kGroup;
+    p.maps = (size_t)p.s.chunks * p.lanes * 16;
+    p.states = (groups * p.lanes * 8 + 15) / 16 * 16;
+    p.tickets = (size_t)p.s.cols * kTicketStride * 4;
+  }
+  p.rows = B * (p.look ? p.s.chunks : 1);
+  p.dpart = backward == 2 ? (size_t)p.rows * 4 * H * 4 : 0;
+  return p;
+}
+
+hipError_t place(Plan& p, LinearArgs& a, void* ws, hipStream_t stream) {
+  char* w = (char*)ws;
+  p.s.maps = (unsigned long long*)w;
+  p.s.states = (unsigned*)(w + p.maps);
+  p.s.tickets = (unsigned*)(w + p.maps + p.states);
+  a.dpart = (float*)(w + p.maps + p.states + p.tickets);
+  if (!p.look) return hipSuccess;
+  const size_t n = (p.maps + p.states) / 16, nt = p.tickets / 16;
+  linear_clear_kernel<<<(unsigned)std::min<size_t>((n + nt + 255) / 256, 1024), 256, 0, stream>>>(
+      (u32x4*)w, n, (u32x4*)p.s.tickets, nt);
+  return hipGetLastError();
+}
+
+// Pairs of units may be read at once: H even, every array of pairs aligned to them.
+bool pairs_aligned(const LinearArgs& a) {
+  const size_t el = a.bf16 ? 2 : 4;
+  uintptr_t o = 0;
+  for (const void* p : {a.p, (const void*)a.h, a.dh, (const void*)a.dp}) o |= (uintptr_t)p % (2 * el);
+  for (const void* p : {(const void*)a.c0, (const void*)a.c_out, (const void*)a.c_save, (const void*)a.dc_out,
+                        (const void*)a.dc0})
+    o |= (uintptr_t)p % 8;
+  return a.H % 2 == 0 && o == 0;
+}
+
+template <class T, bool VEC>
+void launch_run(const LinearArgs& a, const Plan& p, hipStream_t stream) {
+  if (p.walk)
+    linear_walk_kernel<T, VEC><<<(unsigned)((p.lanes + kWalkThreads - 1) / kWalkThreads), kWalkThreads, 0, stream>>>(a);
+  else if (p.look)
+    linear_scan_kernel<T, VEC, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+  else
+    linear_scan_kernel<T, VEC, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
+}
+
+template <class T, bool VEC>
+void launch_back(const LinearArgs& a, const Plan& p, hipStream_t stream) {
+  if (p.look)
+    linear_back_kernel<T, VEC, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+  else
+    linear_back_kernel<T, VEC, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
 }
 
 }  // namespace
 
 size_t linear_workspace(int T, int B, int H, int num_cu, int backward) {
-  (void)T;
-  (void)num_cu;
-  return backward == 2 ? ((size_t)B * 4 * H * 4 + 255) / 256 * 256 : 0;
+  const Plan p = plan_of(T, B, H, num_cu, backward);
+  return p.maps + p.states + p.tickets + p.dpart;
 }
 
-hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
-  (void)ws;
-  const unsigned blocks = (unsigned)(((size_t)a.B * a.H + kWalkThreads - 1) / kWalkThreads);
-  if (a.bf16) linear_walk_kernel<__bf16><<<blocks, kWalkThreads, 0, stream>>>(a);
-  else linear_walk_kernel<float><<<blocks, kWalkThreads, 0, stream>>>(a);
+hipError_t launch_linear(const LinearArgs& a0, void* ws, hipStream_t stream) {
+  LinearArgs a = a0;
+  Plan p = plan_of(a.T, a.B, a.H, a.num_cu, 0);
+  const hipError_t e = place(p, a, ws, stream);
+  if (e != hipSuccess) return e;
+  const bool vec = pairs_aligned(a);
+  if (a.bf16) vec ? launch_run<__bf16, true>(a, p, stream) : launch_run<__bf16, false>(a, p, stream);
+  else vec ? launch_run<float, true>(a, p, stream) : launch_run<float, false>(a, p, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_linear_backward(const LinearArgs& a0, void* ws, hipStream_t stream) {
   LinearArgs a = a0;
-  a.dpart = (float*)ws;
-  const unsigned blocks = (unsigned)(((size_t)a.B * a.H + kWalkThreads - 1) / kWalkThreads);
-  if (a.bf16) linear_back_kernel<__bf16><<<blocks, kWalkThreads, 0, stream>>>(a);
-  else linear_back_kernel<float><<<blocks, kWalkThreads, 0, stream>>>(a);
-  if (a.dbias) linear_dbias_kernel<<<(4 * a.H + 63) / 64, 64, 0, stream>>>(a.dpart, a.B, 4 * a.H, a.dbias);
+  Plan p = plan_of(a.T, a.B, a.H, a.num_cu, a.dbias ? 2 : 1);
+  hipError_t e = place(p, a, ws, stream);
+  if (e != hipSuccess) return e;
+  const bool vec = pairs_aligned(a);
+  if (a.bf16) vec ? launch_back<__bf16, true>(a, p, stream) : launch_back<__bf16, false>(a, p, stream);
+  else vec ? launch_back<float, true>(a, p, stream) : launch_back<float, false>(a, p, stream);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.dbias) return e;
+  linear_dbias_kernel<<<(4 * a.H + 31) / 32, 1024, 0, stream>>>(a.dpart, p.rows, 4 * a.H, a.dbias);
   return hipGetLastError();
 }
 
