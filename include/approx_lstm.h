@@ -537,7 +537,8 @@ void approx_lstm_exact_destroy(approx_lstm_exact* m);
  * Errors: INVALID_ARG for a null p, h_out, dh, c_save (backward) or dp, sizes
  * below those above, a dtype that is neither 0 nor 1, a pointer not aligned to its
  * elements, a workspace missing, too small or not aligned; UNSUPPORTED for a
- * timestep (4 B H elements) of 2 GiB or more and T above 2^31 - 1025.
+ * timestep (4 B H elements) of 2 GiB or more, T above 2^31 - 1025, and a backward
+ * pass of more than 2^22 pieces of 64 timesteps of 128 units.
  */
 #define APPROX_LSTM_LINEAR_SAVE 8
 

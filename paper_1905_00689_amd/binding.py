@@ -7,6 +7,7 @@ module raises at import time rather than falling back to anything.
 """
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -415,75 +416,82 @@ LINEAR_SAVE = 8   # timesteps between two states of c_save
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _on(t, name, shape, dtype, device, optional=False):
-    """Device pointer of a contiguous tensor of that shape and type on `device`."""
-    if t is None:
-        if optional:
-            return None
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
+# the handle of a device's current stream, without the object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on(t, name, shape, dtype, index):
+    """Device pointer of a contiguous tensor of that shape and type on GPU `index`."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+            and t.get_device() == index):
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a torch tensor on the GPU")
-    if t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous {dtype}".replace("torch.", ""))
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return t.data_ptr()
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on GPU {t.get_device()}, not on {index}")
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-class _Launch:
-    """The device of a call's tensors made current, its stream, and workspace
-    from the caller or, for the length of the call, from torch's allocator."""
-
-    def __init__(self, device, stream):
-        self.device, self.stream, self.before = device, stream, None
-
-    def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
-            self.before = torch.cuda.current_device()
-            torch.cuda.set_device(self.device)
-        self.handle = _stream(self.stream)
-        return self
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
-
-    def workspace(self, given, T, B, H, backward):
-        """(tensor or None, pointer, bytes) for a call of these sizes."""
-        if given is not None:
-            if not isinstance(given, torch.Tensor) or not given.is_cuda or not given.is_contiguous():
-                raise TypeError("workspace must be a contiguous torch tensor on the GPU")
-            if given.device != self.device:
-                raise ValueError(f"workspace is on {given.device}, not on {self.device}")
-            return given, given.data_ptr(), given.numel() * given.element_size()
-        n = _linear_workspace(T, B, H, backward)
-        if not n:
-            return None, None, 0
-        if self.handle == torch.cuda.current_stream().cuda_stream:
-            t = torch.empty(n, dtype=torch.uint8, device=self.device)
-        else:   # from the pool of the stream that uses it
-            with torch.cuda.stream(torch.cuda.ExternalStream(self.handle, device=self.device)):
-                t = torch.empty(n, dtype=torch.uint8, device=self.device)
-        return t, t.data_ptr(), n
+def _launch(index, stream, call):
+    """call(stream handle) with GPU `index` current; its status checked.  stream:
+    None (the current one of that GPU), a torch stream or a handle."""
+    before = torch.cuda.current_device()
+    if before == index:
+        status = call(_raw_stream(index) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            status = call(_raw_stream(index) if stream is None else _stream(stream))
+    if status != OK:
+        _check(status)
+    return status
 
 
-def _linear_workspace(T, B, H, backward):
+@functools.lru_cache(maxsize=4096)
+def _linear_workspace(T, B, H, backward, index):
     n = ctypes.c_uint64()
-    _check(lib.approx_lstm_linear_workspace(T, B, H, backward, ctypes.byref(n)))
+    with torch.cuda.device(index):
+        _check(lib.approx_lstm_linear_workspace(T, B, H, backward, ctypes.byref(n)))
     return n.value
 
 
+def _linear_call(function, T, B, H, backward, index, workspace, stream, args):
+    """function(*args, workspace, its bytes, stream) with workspace from the caller
+    or, for the length of the call, from torch's allocator."""
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous torch tensor on the GPU")
+        if workspace.get_device() != index:
+            raise ValueError(f"workspace is on GPU {workspace.get_device()}, not on {index}")
+        at, n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        return _launch(index, stream, lambda s: function(*args, at, n, s))
+    n = _linear_workspace(T, B, H, backward, index)
+    if not n:
+        return _launch(index, stream, lambda s: function(*args, None, 0, s))
+
+    def call(s):
+        if s == _raw_stream(index):
+            ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{index}")
+        else:   # from the pool of the stream that uses it
+            with torch.cuda.stream(torch.cuda.ExternalStream(s, device=index)):
+                ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{index}")
+        return function(*args, ws.data_ptr(), n, s)
+
+    return _launch(index, stream, call)
+
+
 def _gates(p):
-    """(T, B, H, device, dtype code) of pre-activations p [T, B, 4H]."""
+    """(T, B, H, GPU, dtype code) of pre-activations p [T, B, 4H]."""
     if not isinstance(p, torch.Tensor) or not p.is_cuda:
         raise TypeError("p must be a torch tensor on the GPU")
     if p.dtype not in _DTYPES or not p.is_contiguous():
         raise TypeError("p must be contiguous float32 or bfloat16")
-    if p.dim() != 3 or p.shape[2] % 4 or not p.shape[2]:
-        raise ValueError(f"p has shape {tuple(p.shape)}, expected (T, B, 4 H)")
-    return p.shape[0], p.shape[1], p.shape[2] // 4, p.device, _DTYPES[p.dtype]
+    shape = p.shape
+    if len(shape) != 3 or shape[2] % 4 or not shape[2] or not shape[1]:
+        raise ValueError(f"p has shape {tuple(shape)}, expected (T, B, 4 H)")
+    return shape[0], shape[1], shape[2] // 4, p.get_device(), _DTYPES[p.dtype]
 
 
 def approx_lstm_linear_run(p, h_out, bias=None, lengths=None, c0=None, c_out=None, c_save=None, workspace=None,
@@ -492,16 +500,15 @@ def approx_lstm_linear_run(p, h_out, bias=None, lengths=None, c0=None, c_out=Non
     bfloat16; bias [4H], c0, c_out [B, H], c_save [ceil(T / 8), B, H] float32,
     lengths [B] int32, or None.  workspace: a GPU tensor of at least
     approx_lstm_linear_workspace(T, B, H) bytes, or None (taken from torch)."""
-    T, B, H, dev, dt = _gates(p)
+    T, B, H, at, dt = _gates(p)
     f32 = torch.float32
-    with _Launch(dev, stream) as call:
-        ws, wp, wn = call.workspace(workspace, T, B, H, 0)
-        st = lib.approx_lstm_linear_run(
-            p.data_ptr(), _on(bias, "bias", (4 * H,), f32, dev, True), T, B, H, dt,
-            _on(lengths, "lengths", (B,), torch.int32, dev, True), _on(c0, "c0", (B, H), f32, dev, True),
-            _on(h_out, "h_out", (T, B, H), p.dtype, dev), _on(c_out, "c_out", (B, H), f32, dev, True),
-            _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, dev, True), wp, wn, call.handle)
-    return _check(st)
+    return _linear_call(
+        lib.approx_lstm_linear_run, T, B, H, 0, at, workspace, stream,
+        (p.data_ptr(), None if bias is None else _on(bias, "bias", (4 * H,), f32, at), T, B, H, dt,
+         None if lengths is None else _on(lengths, "lengths", (B,), torch.int32, at),
+         None if c0 is None else _on(c0, "c0", (B, H), f32, at), _on(h_out, "h_out", (T, B, H), p.dtype, at),
+         None if c_out is None else _on(c_out, "c_out", (B, H), f32, at),
+         None if c_save is None else _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, at)))
 
 
 def approx_lstm_linear_backward(p, dh, c_save, dp, bias=None, lengths=None, dc_out=None, dc0=None, dbias=None,
@@ -509,25 +516,24 @@ def approx_lstm_linear_backward(p, dh, c_save, dp, bias=None, lengths=None, dc_o
     """Gradients of the gated linear recurrence: dp [T, B, 4H], dc0 [B, H] and
     dbias [4H] (None: not wanted) from dh [T, B, H] and dc_out [B, H] (None:
     zeros), with the run's p, bias, lengths and c_save."""
-    T, B, H, dev, dt = _gates(p)
+    T, B, H, at, dt = _gates(p)
     f32 = torch.float32
-    with _Launch(dev, stream) as call:
-        ws, wp, wn = call.workspace(workspace, T, B, H, 1 if dbias is None else 2)
-        st = lib.approx_lstm_linear_backward(
-            p.data_ptr(), _on(bias, "bias", (4 * H,), f32, dev, True), T, B, H, dt,
-            _on(lengths, "lengths", (B,), torch.int32, dev, True),
-            _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, dev),
-            _on(dh, "dh", (T, B, H), p.dtype, dev), _on(dc_out, "dc_out", (B, H), f32, dev, True),
-            _on(dp, "dp", (T, B, 4 * H), p.dtype, dev), _on(dc0, "dc0", (B, H), f32, dev, True),
-            _on(dbias, "dbias", (4 * H,), f32, dev, True), wp, wn, call.handle)
-    return _check(st)
+    return _linear_call(
+        lib.approx_lstm_linear_backward, T, B, H, 1 if dbias is None else 2, at, workspace, stream,
+        (p.data_ptr(), None if bias is None else _on(bias, "bias", (4 * H,), f32, at), T, B, H, dt,
+         None if lengths is None else _on(lengths, "lengths", (B,), torch.int32, at),
+         _on(c_save, "c_save", ((T + LINEAR_SAVE - 1) // LINEAR_SAVE, B, H), f32, at),
+         _on(dh, "dh", (T, B, H), p.dtype, at), None if dc_out is None else _on(dc_out, "dc_out", (B, H), f32, at),
+         _on(dp, "dp", (T, B, 4 * H), p.dtype, at), None if dc0 is None else _on(dc0, "dc0", (B, H), f32, at),
+         None if dbias is None else _on(dbias, "dbias", (4 * H,), f32, at)))
 
 
 def approx_lstm_linear_workspace(T, B, H, backward=0, device=None):
     """Bytes of workspace of a run (backward 0) or of a backward pass without (1)
     or with dbias (2), on `device` (None: the current one)."""
-    with _Launch(torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device), 0):
-        return _linear_workspace(int(T), int(B), int(H), int(backward))
+    device = torch.device("cuda" if device is None else device)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    return _linear_workspace(int(T), int(B), int(H), int(backward), index)
 
 
 class Q4Matrix:
@@ -551,7 +557,7 @@ def approx_lstm_q4_prepare(w, group=128, stream=None):
         raise ValueError(f"w has shape {w.shape}, expected (rows, cols)")
     out = ctypes.c_void_p()
     _check(lib.approx_lstm_q4_prepare(wp, *w.shape, int(group), _stream(stream), ctypes.byref(out)))
-    return Q4Matrix(out.value, *w.shape, int(group), torch.device("cuda", torch.cuda.current_device()))
+    return Q4Matrix(out.value, *w.shape, int(group), torch.cuda.current_device())
 
 
 def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):
@@ -560,16 +566,14 @@ def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):
     (None: 8): GPU tensors; returns a Q4Matrix."""
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 2:
         raise TypeError("q must be a torch tensor [rows, ceil(cols / 2)] on the GPU")
-    cols, group = int(cols), int(group)
-    rows, dev, groups = q.shape[0], q.device, -(-cols // group) if group > 0 else 0
+    cols, group, index = int(cols), int(group), q.get_device()
+    rows, groups = q.shape[0], -(-cols // group) if group > 0 else 0
     out = ctypes.c_void_p()
-    with _Launch(dev, stream) as call:
-        _check(lib.approx_lstm_q4_load(
-            _on(q, "q", (rows, (cols + 1) // 2), torch.uint8, dev),
-            _on(scale, "scale", (rows, groups), torch.float32, dev),
-            _on(zero, "zero", (rows, groups), torch.uint8, dev, True), rows, cols, group, call.handle,
-            ctypes.byref(out)))
-    return Q4Matrix(out.value, rows, cols, group, dev)
+    at = (_on(q, "q", (rows, (cols + 1) // 2), torch.uint8, index),
+          _on(scale, "scale", (rows, groups), torch.float32, index),
+          None if zero is None else _on(zero, "zero", (rows, groups), torch.uint8, index))
+    _launch(index, stream, lambda s: lib.approx_lstm_q4_load(*at, rows, cols, group, s, ctypes.byref(out)))
+    return Q4Matrix(out.value, rows, cols, group, index)
 
 
 def approx_lstm_q4_get(m, stream=None):
@@ -579,8 +583,8 @@ def approx_lstm_q4_get(m, stream=None):
     q = np.empty((m.rows, (m.cols + 1) // 2), np.uint8)
     s = np.empty((m.rows, groups), np.float32)
     z = np.empty((m.rows, groups), np.uint8)
-    with _Launch(m.device, stream) as call:
-        _check(lib.approx_lstm_q4_get(m.handle, q.ctypes.data, s.ctypes.data, z.ctypes.data, call.handle))
+    _launch(m.device, stream,
+            lambda st: lib.approx_lstm_q4_get(m.handle, q.ctypes.data, s.ctypes.data, z.ctypes.data, st))
     return dict(q=q, scale=s, zero=z)
 
 
@@ -591,9 +595,8 @@ def approx_lstm_q4_run(m, x, y, bias=None, stream=None):
         raise TypeError("x must be a torch tensor [N, cols] on the GPU")
     if x.dtype not in _DTYPES:
         raise TypeError("x must be float32 or bfloat16")
-    N, dev = x.shape[0], m.device
-    with _Launch(dev, stream) as call:
-        st = lib.approx_lstm_q4_run(
-            m.handle, _on(x, "x", (N, m.cols), x.dtype, dev), N, _DTYPES[x.dtype],
-            _on(bias, "bias", (m.rows,), torch.float32, dev, True), _on(y, "y", (N, m.rows), x.dtype, dev), call.handle)
-    return _check(st)
+    N, at = x.shape[0], m.device
+    args = (m.handle, _on(x, "x", (N, m.cols), x.dtype, at), N, _DTYPES[x.dtype],
+            None if bias is None else _on(bias, "bias", (m.rows,), torch.float32, at),
+            _on(y, "y", (N, m.rows), x.dtype, at))
+    return _launch(at, stream, lambda s: lib.approx_lstm_q4_run(*args, s))

@@ -1724,6 +1724,8 @@ approx_lstm_status check_linear(alstm::LinearArgs& a, int dtype, int backward, c
   a.bf16 = dtype;
   approx_lstm_status st = current_cus(&a.num_cu);
   if (st != APPROX_LSTM_OK) return st;
+  if (!alstm::linear_fits(a.T, a.B, a.H, a.num_cu, backward))
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "a backward pass of more than 2^22 pieces of 64 timesteps of 128 units");
   const size_t need = alstm::linear_workspace(a.T, a.B, a.H, a.num_cu, backward);
   if (need && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(APPROX_LSTM_ERR_INVALID_ARG, "workspace of %zu bytes, 16-byte aligned, needed (given: %llu)", need,

@@ -11,6 +11,7 @@
 // its 8 steps from its own first state, so p is read once and nothing but maps is
 // exchanged.  Every composition has a fixed order: same bits whatever runs beside.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "gated.hpp"
@@ -30,70 +31,72 @@ constexpr int kSteps = kLinearSave;            // timesteps of a wave
 constexpr int kScanWaves = 8;
 constexpr int kScanThreads = 64 * kScanWaves;
 constexpr int kChunk = kSteps * kScanWaves;    // timesteps of a workgroup at once
-constexpr int kGroup = 32;                     // chunks between two handed-on states
-constexpr int kPolls = kGroup / kScanWaves;    // maps a wave collects
+constexpr int kGroup = kScanWaves * kScanWaves;   // chunks between two handed-on states
 constexpr int kTicketStride = 16;              // words between two columns' tickets (64 bytes)
 constexpr int kWalkThreads = 256;
+constexpr size_t kMostChunks = 1u << 22;       // of all columns, where chunks hand over
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Two neighbouring units of a row.  VEC: both there (H even) and the pair aligned;
-// else read one by one, `two` false where the second is past the row (it then
-// reads the first again).
+// Two neighbouring units of a row, loaded and stored at once at any alignment of
+// their elements.  With an odd number of units the last lane of a row has one
+// (`two` false): it loads the unit before as well and swaps, so nothing past the row
+// is touched, and stores it alone.  Rows of a single unit go one by one.
+enum Rows { kEven, kOdd, kSingle };
+
 template <class T>
 struct Pair;
 template <>
 struct Pair<float> {
   typedef f32x2 Raw;
+  typedef f32x2 Any __attribute__((aligned(4)));
   static __device__ __forceinline__ f32x2 get(Raw r) { return r; }
   static __device__ __forceinline__ Raw put(f32x2 v) { return v; }
-  static __device__ __forceinline__ Raw join(const float* p, bool two) { return Raw{p[0], p[two ? 1 : 0]}; }
-  static __device__ __forceinline__ void split(float* p, Raw r, bool two) {
-    p[0] = r[0];
-    if (two) p[1] = r[1];
-  }
+  static __device__ __forceinline__ Raw one(float v) { return Raw{v, v}; }
+  static __device__ __forceinline__ Raw swap(Raw r) { return Raw{r[1], r[0]}; }
+  static __device__ __forceinline__ float low(Raw r) { return r[0]; }
 };
 template <>
 struct Pair<__bf16> {
   typedef unsigned Raw;
+  typedef unsigned Any __attribute__((aligned(2)));
   static __device__ __forceinline__ f32x2 get(Raw r) {
     return f32x2{__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u)};
   }
   static __device__ __forceinline__ Raw put(f32x2 v) {
     return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));   // to the nearest, ties to even
   }
-  static __device__ __forceinline__ Raw join(const __bf16* p, bool two) {
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-    return (unsigned)q[0] | ((unsigned)q[two ? 1 : 0] << 16);
-  }
-  static __device__ __forceinline__ void split(__bf16* p, Raw r, bool two) {
-    uint16_t* q = reinterpret_cast<uint16_t*>(p);
-    q[0] = (uint16_t)r;
-    if (two) q[1] = (uint16_t)(r >> 16);
-  }
+  static __device__ __forceinline__ Raw one(__bf16 v) { return __builtin_bit_cast(uint16_t, v); }
+  static __device__ __forceinline__ Raw swap(Raw r) { return r >> 16; }
+  static __device__ __forceinline__ __bf16 low(Raw r) { return __builtin_bit_cast(__bf16, (uint16_t)r); }
 };
 
-template <class T, bool VEC>
+template <class T, Rows R>
 __device__ __forceinline__ typename Pair<T>::Raw load_pair(const char* row, unsigned off, bool two) {
-  const T* p = reinterpret_cast<const T*>(row + off);
-  if constexpr (VEC) return *reinterpret_cast<const typename Pair<T>::Raw*>(p);
-  else return Pair<T>::join(p, two);
+  if constexpr (R == kSingle) {
+    return Pair<T>::one(*reinterpret_cast<const T*>(row + off));
+  } else if constexpr (R == kOdd) {
+    const typename Pair<T>::Raw r =
+        *reinterpret_cast<const typename Pair<T>::Any*>(row + (off - (two ? 0u : (unsigned)sizeof(T))));
+    return two ? r : Pair<T>::swap(r);
+  } else {
+    return *reinterpret_cast<const typename Pair<T>::Any*>(row + off);
+  }
 }
 
-template <class T, bool VEC>
+template <class T, Rows R>
 __device__ __forceinline__ void store_pair(char* row, unsigned off, f32x2 v, bool two) {
-  T* p = reinterpret_cast<T*>(row + off);
   const auto r = Pair<T>::put(v);
-  if constexpr (VEC) *reinterpret_cast<typename Pair<T>::Raw*>(p) = r;
-  else Pair<T>::split(p, r, two);
+  if (R == kEven || (R == kOdd && two)) *reinterpret_cast<typename Pair<T>::Any*>(row + off) = r;
+  else *reinterpret_cast<T*>(row + off) = Pair<T>::low(r);
 }
 
-template <bool VEC>
-__device__ __forceinline__ f32x2 load_state(const float* p, bool two) {
-  return load_pair<float, VEC>(reinterpret_cast<const char*>(p), 0, two);
+template <Rows R>
+__device__ __forceinline__ f32x2 load_state(const float* p, unsigned at, bool two) {
+  return load_pair<float, R>(reinterpret_cast<const char*>(p), at * 4u, two);
 }
-template <bool VEC>
-__device__ __forceinline__ void store_state(float* p, f32x2 v, bool two) {
-  store_pair<float, VEC>(reinterpret_cast<char*>(p), 0, v, two);
+template <Rows R>
+__device__ __forceinline__ void store_state(float* p, unsigned at, f32x2 v, bool two) {
+  store_pair<float, R>(reinterpret_cast<char*>(p), at * 4u, v, two);
 }
 
 // What a lane works on: units r, r + 1 of sequence b.
@@ -123,11 +126,9 @@ struct GateBias {
   f32x2 i, f, g, o;
 };
 
-template <bool VEC>
 __device__ __forceinline__ GateBias gate_bias(const LinearArgs& a, const Lane& l) {
   GateBias b{};
   if (a.bias) {
-    // (the bias need be aligned to its elements only)
     auto at = [&](int q) {
       const float* p = a.bias + (size_t)q * a.H + l.r;
       return f32x2{p[0], p[l.two ? 1 : 0]};
@@ -154,29 +155,29 @@ __device__ __forceinline__ float gate_tanh(float x, float b) {
 
 // Few timesteps: a lane walks its two units through all of them, the loads of
 // kAhead timesteps at once.
-template <class T, bool VEC>
+template <class T, Rows R>
 __global__ void __launch_bounds__(kWalkThreads) linear_walk_kernel(LinearArgs a) {
   constexpr int kAhead = 4;
   const Lane l = lane_of(a, blockIdx.x * kWalkThreads + threadIdx.x);
   if (!l.live) return;
-  const GateBias bias = gate_bias<VEC>(a, l);
+  const GateBias bias = gate_bias(a, l);
   const size_t BH = (size_t)a.B * a.H;
   const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T);
-  f32x2 c = a.c0 ? load_state<VEC>(a.c0 + l.at, l.two) : f32x2{0.f, 0.f};
+  f32x2 c = a.c0 ? load_state<R>(a.c0, l.at, l.two) : f32x2{0.f, 0.f};
   for (int t0 = 0; t0 < a.T; t0 += kAhead) {
     typename Pair<T>::Raw raw[kAhead][4];
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
       const char* row = (const char*)a.p + (size_t)min(t0 + s, a.T - 1) * (4 * BH * sizeof(T));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) raw[s][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
+      for (int q = 0; q < 4; ++q) raw[s][q] = load_pair<T, R>(row, ga + q * gs, l.two);
     }
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
       const int t = t0 + s;
       if (t >= a.T) break;
       if (s % kSteps == 0 && t % kSteps == 0 && a.c_save)
-        store_state<VEC>(a.c_save + (size_t)(t / kSteps) * BH + l.at, c, l.two);
+        store_state<R>(a.c_save + (size_t)(t / kSteps) * BH, l.at, c, l.two);
       const f32x2 yi = Pair<T>::get(raw[s][0]), yf = Pair<T>::get(raw[s][1]), yg = Pair<T>::get(raw[s][2]),
                   yo = Pair<T>::get(raw[s][3]);
       f32x2 h{0.f, 0.f};
@@ -187,10 +188,10 @@ __global__ void __launch_bounds__(kWalkThreads) linear_walk_kernel(LinearArgs a)
           h[k] = gate_sig(yo[k], bias.o[k]) * gate_tanh(c[k], 0.f);
         }
       }
-      store_pair<T, VEC>((char*)a.h + (size_t)t * (BH * sizeof(T)), l.at * sizeof(T), h, l.two);
+      store_pair<T, R>((char*)a.h + (size_t)t * (BH * sizeof(T)), l.at * sizeof(T), h, l.two);
     }
   }
-  if (a.c_out) store_state<VEC>(a.c_out + l.at, c, l.two);
+  if (a.c_out) store_state<R>(a.c_out, l.at, c, l.two);
 }
 
 // A map c -> A c + B of two units, {A0, B0, A1, B1}.
@@ -207,9 +208,12 @@ constexpr f32x4 kIdentity{1.f, 0.f, 1.f, 0.f};
 // device and so its chunks run side by side.  A word is empty (all ones, as the
 // kernel before cleared it) until its value is there; a value with the bits of an
 // empty word is written as another NaN.  A chunk publishes its map as soon as it
-// has it, collects the maps of the chunks before it in its group of kGroup, and
-// waits for the one state that the group before handed on; the last chunk of a
-// group hands on its own.  So a hop of the serial chain passes kGroup chunks.
+// has it; the last of kScanWaves chunks, a block, publishes the block's instead.
+// Each wave collects one map of an earlier chunk of the block and one of an earlier
+// block of the group (kScanWaves blocks, 4096 timesteps), and one waits for the
+// state that the group before handed on: a hop of the serial chain passes a whole
+// group, and a chunk reads 7 maps on average.  (One level of 32 chunks, 16 maps on
+// average, took 121 us instead of 113 at T = 65536, H = 512, bf16.)
 //
 // Which chunk a workgroup takes is the ticket of its column: in the order in which
 // workgroups start, so the chunks that anyone waits for have workgroups that run.
@@ -231,9 +235,19 @@ __device__ __forceinline__ void publish_state(unsigned* w, const f32x2& c) {
     __hip_atomic_store(w + k, filled(c[k]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Lane 0 (of a wave with work, its lane too) looks until its word is there, so that a
+// wave that waits asks for one line and not for sixteen.
+__device__ __forceinline__ unsigned await_first(const unsigned* w) {
+  unsigned spins = 0;
+  if ((threadIdx.x & 63) == 0)
+    while (__hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == kEmpty && ++spins < kSpinLimit)
+      __builtin_amdgcn_s_sleep(8);
+  return __builtin_amdgcn_readfirstlane(spins);
+}
+
 // the state of a word pair; NaN past the spin limit
 __device__ __forceinline__ f32x2 await_state(const unsigned* w) {
-  unsigned v[2], spins = 0;
+  unsigned v[2], spins = await_first(w);
   while (true) {
     v[0] = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     v[1] = __hip_atomic_load(w + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -243,37 +257,26 @@ __device__ __forceinline__ f32x2 await_state(const unsigned* w) {
   return f32x2{__uint_as_float(v[0]), __uint_as_float(v[1])};   // (an empty word is a NaN)
 }
 
-// the composition of n (1 .. kPolls) maps, `stride` words apart; NaN past the limit
-__device__ __forceinline__ f32x4 await_maps(const unsigned long long* w, size_t stride, int n) {
-  unsigned long long v[kPolls][2];
-  unsigned spins = 0;
+// a published map; NaN past the spin limit
+__device__ __forceinline__ f32x4 await_map(const unsigned long long* w) {
+  unsigned long long v[2];
+  unsigned spins = await_first(reinterpret_cast<const unsigned*>(w) + 1);
   while (true) {
-    bool all = true;
-#pragma unroll
-    for (int j = 0; j < kPolls; ++j)
-      if (j < n)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          v[j][k] = __hip_atomic_load(w + j * stride + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-    for (int j = 0; j < kPolls; ++j)
-      if (j < n) all = all && (unsigned)(v[j][0] >> 32) != kEmpty && (unsigned)(v[j][1] >> 32) != kEmpty;
-    if (all || ++spins >= kSpinLimit) break;
+    v[0] = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v[1] = __hip_atomic_load(w + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (((unsigned)(v[0] >> 32) != kEmpty && (unsigned)(v[1] >> 32) != kEmpty) || ++spins >= kSpinLimit) break;
     __builtin_amdgcn_s_sleep(1);
   }
-  f32x4 m = kIdentity;
-#pragma unroll
-  for (int j = 0; j < kPolls; ++j)
-    if (j < n)
-      m = then(m, f32x4{__uint_as_float((unsigned)(v[j][0] >> 32)), __uint_as_float((unsigned)v[j][0]),
-                        __uint_as_float((unsigned)(v[j][1] >> 32)), __uint_as_float((unsigned)v[j][1])});
-  return m;
+  return f32x4{__uint_as_float((unsigned)(v[0] >> 32)), __uint_as_float((unsigned)v[0]),
+               __uint_as_float((unsigned)(v[1] >> 32)), __uint_as_float((unsigned)v[1])};
 }
 
 struct ScanLds {
   f32x4 wave[2][kScanWaves][64];   // maps of the waves (of even and odd rounds)
-  f32x4 before[kScanWaves][64];    // maps that the waves collected
-  f32x2 entry[64];                 // the state that the group begins with
+  f32x4 chunks[kScanWaves][64];    // maps of the chunks before in the block
+  f32x4 blocks[kScanWaves][64];    // maps of the blocks before in the group
+  f32x4 total[64];                 // map of the chunk
+  f32x2 entry[64];                 // the state that the chunk begins with
   int ticket;
 };
 
@@ -285,53 +288,55 @@ struct ScanLds {
 template <class Load>
 __device__ __forceinline__ f32x2 hand_over(ScanLds& lds, const LinearScan& s, int order, int wave_order, int lane,
                                            size_t idx, bool live, Load first) {
-  const int g = order / kGroup, r = order - g * kGroup;
+  const int block = order / kScanWaves, i = order % kScanWaves, group = block / kScanWaves, j = block % kScanWaves;
   const bool last = order + 1 >= s.chunks;
   const size_t stride = 2 * (size_t)s.lanes;
-  if (wave_order == kScanWaves - 1 && !last && r != kGroup - 1) {
+  if (wave_order == kScanWaves - 1) {
     f32x4 m = lds.wave[0][0][lane];
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < kScanWaves; ++w) m = then(m, lds.wave[0][w][lane]);
-    if (live) publish_map(s.maps + order * stride + 2 * idx, m);
+    lds.total[lane] = m;
+    if (live && !last && i != kScanWaves - 1) publish_map(s.maps + order * stride + 2 * idx, m);
   }
-  const int have = r - kPolls * wave_order;   // maps before this chunk that are left to this wave
-  if (have > 0)
-    lds.before[wave_order][lane] =
-        live ? await_maps(s.maps + (size_t)(g * kGroup + kPolls * wave_order) * stride + 2 * idx, stride, min(have, kPolls))
-             : kIdentity;
+  if (wave_order < i && live)
+    lds.chunks[wave_order][lane] = await_map(s.maps + (size_t)(order - i + wave_order) * stride + 2 * idx);
+  lds_barrier();
+  if (wave_order == kScanWaves - 1 && i == kScanWaves - 1 && j != kScanWaves - 1 && !last) {
+    f32x4 m = lds.chunks[0][lane];
+#pragma unroll 1
+    for (int w = 1; w < i; ++w) m = then(m, lds.chunks[w][lane]);
+    if (live) publish_map(s.maps + (s.chunks + block) * stride + 2 * idx, then(m, lds.total[lane]));
+  }
+  if (wave_order < j && live)
+    lds.blocks[wave_order][lane] = await_map(s.maps + (size_t)(s.chunks + block - j + wave_order) * stride + 2 * idx);
   lds_barrier();
   if (wave_order == 0) {
-    f32x4 m = kIdentity;
-    const bool hands_on = r == kGroup - 1 && !last;
-    if (hands_on) {   // composed before the state comes, one step when it is there
-#pragma unroll
-      for (int w = 0; w < kScanWaves; ++w)
-        if (kPolls * w < r) m = then(m, lds.before[w][lane]);
-#pragma unroll
-      for (int w = 0; w < kScanWaves; ++w) m = then(m, lds.wave[0][w][lane]);
-    }
+    f32x4 m = kIdentity;   // from the group's first state to this chunk's
+#pragma unroll 1
+    for (int w = 0; w < j; ++w) m = then(m, lds.blocks[w][lane]);
+#pragma unroll 1
+    for (int w = 0; w < i; ++w) m = then(m, lds.chunks[w][lane]);
+    const bool hands_on = i == kScanWaves - 1 && j == kScanWaves - 1 && !last;
+    f32x4 through = m;
+    if (hands_on) through = then(m, lds.total[lane]);
     f32x2 c{0.f, 0.f};
     if (order == 0) {
       c = first();
       if (live && !last) publish_state(s.states + 2 * idx, c);
     } else if (live) {
-      c = await_state(s.states + g * stride + 2 * idx);
+      c = await_state(s.states + group * stride + 2 * idx);
     }
-    if (hands_on && live) publish_state(s.states + (g + 1) * stride + 2 * idx, apply(m, c));
-    lds.entry[lane] = c;
+    if (hands_on && live) publish_state(s.states + (group + 1) * stride + 2 * idx, apply(through, c));
+    lds.entry[lane] = apply(m, c);
   }
   lds_barrier();
-  f32x2 c = lds.entry[lane];
-#pragma unroll
-  for (int w = 0; w < kScanWaves; ++w)
-    if (kPolls * w < r) c = apply(lds.before[w][lane], c);
-  return c;
+  return lds.entry[lane];
 }
 
 // LOOK: a workgroup takes one chunk and chunks hand over; else it takes its
 // column's chunks one after another and keeps the state.
-template <class T, bool VEC, bool LOOK>
-__global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs a, LinearScan s) {
+template <class T, Rows R, bool LOOK>
+__global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T) == 4) ? 6 : 4) linear_scan_kernel(LinearArgs a, LinearScan s) {
   __shared__ ScanLds lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int col = blockIdx.x, chunk = 0;
@@ -345,34 +350,34 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs
   }
   const int idx = col * 64 + lane;
   const Lane l = lane_of(a, idx);
-  const GateBias bias = gate_bias<VEC>(a, l);
+  const GateBias bias = gate_bias(a, l);
   const size_t BH = (size_t)a.B * a.H;
   const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T), ha = l.at * sizeof(T);
-  auto first = [&] { return a.c0 ? load_state<VEC>(a.c0 + l.at, l.two) : f32x2{0.f, 0.f}; };
+  auto first = [&] { return a.c0 ? load_state<R>(a.c0, l.at, l.two) : f32x2{0.f, 0.f}; };
   if (!LOOK && wave == 0) lds.entry[lane] = first();   // (one wave reads it: c_out may be c0)
   f32x2 carry{0.f, 0.f};
   for (; chunk < s.chunks; ++chunk) {
     const int t0 = chunk * kChunk + wave * kSteps;
-    typename Pair<T>::Raw raw[kSteps][4];
+    const int n = min(l.len - t0, kSteps);   // timesteps here that the sequence has
+    const bool some = __any(n > 0);          // (a wave of padding alone loads nothing)
+    typename Pair<T>::Raw raw[kSteps][4] = {};
+    if (some)
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const char* row = (const char*)a.p + (size_t)min(t0 + k, a.T - 1) * (4 * BH * sizeof(T));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, R>(row, ga + q * gs, l.two);
+      }
+    f32x2 f[kSteps], u[kSteps];
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
-      const char* row = (const char*)a.p + (size_t)min(t0 + k, a.T - 1) * (4 * BH * sizeof(T));
-#pragma unroll
-      for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
-    }
-    f32x2 f[kSteps], u[kSteps], o[kSteps];
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]),
-                  yo = Pair<T>::get(raw[k][3]);
+      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         f[k][j] = gate_forget(yf[j], bias.f[j]);
         u[k][j] = gate_sig(yi[j], bias.i[j]) * gate_tanh(yg[j], bias.g[j]);
-        o[k][j] = gate_sig(yo[j], bias.o[j]);
       }
     }
-    const int n = min(l.len - t0, kSteps);   // timesteps here that the sequence has
     if (a.lengths || t0 + kSteps > a.T) {
 #pragma unroll
       for (int k = 0; k < kSteps; ++k)
@@ -386,7 +391,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs
     lds_barrier();
     f32x2 c = !LOOK && chunk == 0 ? lds.entry[lane] : carry;
     if constexpr (LOOK) c = hand_over(lds, s, chunk, wave, lane, idx, l.live, first);
-#pragma unroll
+#pragma unroll 2
     for (int w = 0; w < kScanWaves; ++w) {
       if (w == wave) carry = c;
       if (LOOK && w == wave) break;
@@ -396,19 +401,20 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs
     c = carry;          // the wave's first state
     carry = next;       // the chunk's last one
     if (l.live) {
-      if (a.c_save && t0 < a.T) store_state<VEC>(a.c_save + (size_t)(t0 / kSteps) * BH + l.at, c, l.two);
+      if (a.c_save && t0 < a.T) store_state<R>(a.c_save + (size_t)(t0 / kSteps) * BH, l.at, c, l.two);
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
         f32x2 h;
+        const f32x2 yo = Pair<T>::get(raw[k][3]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           c[j] = __builtin_fmaf(f[k][j], c[j], u[k][j]);
-          h[j] = o[k][j] * gate_tanh(c[j], 0.f);
+          h[j] = gate_sig(yo[j], bias.o[j]) * gate_tanh(c[j], 0.f);
           if (k >= n) h[j] = 0.f;
         }
-        if (t0 + k < a.T) store_pair<T, VEC>((char*)a.h + (size_t)(t0 + k) * (BH * sizeof(T)), ha, h, l.two);
+        if (t0 + k < a.T) store_pair<T, R>((char*)a.h + (size_t)(t0 + k) * (BH * sizeof(T)), ha, h, l.two);
       }
-      if (a.c_out && chunk == s.chunks - 1 && wave == kScanWaves - 1) store_state<VEC>(a.c_out + l.at, c, l.two);
+      if (a.c_out && chunk == s.chunks - 1 && wave == kScanWaves - 1) store_state<R>(a.c_out, l.at, c, l.two);
     }
     if constexpr (LOOK) break;
   }
@@ -422,7 +428,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_scan_kernel(LinearArgs
 // A wave runs its 8 steps forward from the saved state, so c is neither stored nor
 // read but every 8 timesteps, and keeps f, w and the three factors of d; its map is
 // e -> A e + B again.  The sums of dp over its timesteps leave through dpart.
-template <class T, bool VEC, bool LOOK>
+template <class T, Rows R, bool LOOK>
 __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs a, LinearScan s) {
   __shared__ ScanLds lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -437,11 +443,11 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
   }
   const int idx = col * 64 + lane;
   const Lane l = lane_of(a, idx);
-  const GateBias bias = gate_bias<VEC>(a, l);
+  const GateBias bias = gate_bias(a, l);
   const size_t BH = (size_t)a.B * a.H;
   const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T), ha = l.at * sizeof(T);
   const int place = kScanWaves - 1 - wave;   // the wave's place in the order of the pass
-  auto first = [&] { return a.dc_out ? load_state<VEC>(a.dc_out + l.at, l.two) : f32x2{0.f, 0.f}; };
+  auto first = [&] { return a.dc_out ? load_state<R>(a.dc_out, l.at, l.two) : f32x2{0.f, 0.f}; };
   if (!LOOK && place == 0) lds.entry[lane] = first();   // (one wave reads it: dc0 may be dc_out)
   f32x2 carry{0.f, 0.f};
   f32x2 si{0.f, 0.f}, sf = si, sg = si, so = si;
@@ -453,10 +459,10 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
       const size_t t = (size_t)min(t0 + k, a.T - 1);
       const char* row = (const char*)a.p + t * (4 * BH * sizeof(T));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, VEC>(row, ga + q * gs, l.two);
-      rdh[k] = load_pair<T, VEC>((const char*)a.dh + t * (BH * sizeof(T)), ha, l.two);
+      for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, R>(row, ga + q * gs, l.two);
+      rdh[k] = load_pair<T, R>((const char*)a.dh + t * (BH * sizeof(T)), ha, l.two);
     }
-    f32x2 c = load_state<VEC>(a.c_save + (size_t)(min(t0, a.T - 1) / kSteps) * BH + l.at, l.two);
+    f32x2 c = load_state<R>(a.c_save + (size_t)(min(t0, a.T - 1) / kSteps) * BH, l.at, l.two);
     const int n = min(l.len - t0, kSteps);
     f32x2 f[kSteps], w[kSteps], ki[kSteps], kf[kSteps], kg[kSteps];
 #pragma unroll
@@ -480,7 +486,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
         so[j] += dO[j];
       }
       if (l.live && t0 + k < a.T)
-        store_pair<T, VEC>((char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T)), ga + 3 * gs, dO, l.two);
+        store_pair<T, R>((char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T)), ga + 3 * gs, dO, l.two);
     }
     f32x4 m = kIdentity;
 #pragma unroll
@@ -491,7 +497,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
     lds_barrier();
     f32x2 e = !LOOK && order == 0 ? lds.entry[lane] : carry;
     if constexpr (LOOK) e = hand_over(lds, s, order, place, lane, idx, l.live, first);
-#pragma unroll
+#pragma unroll 2
     for (int v = 0; v < kScanWaves; ++v) {
       if (v == place) carry = e;
       if (LOOK && v == place) break;
@@ -512,12 +518,12 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
       }
       if (l.live && t0 + k < a.T) {
         char* row = (char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T));
-        store_pair<T, VEC>(row, ga, di, l.two);
-        store_pair<T, VEC>(row, ga + gs, df, l.two);
-        store_pair<T, VEC>(row, ga + 2 * gs, dg, l.two);
+        store_pair<T, R>(row, ga, di, l.two);
+        store_pair<T, R>(row, ga + gs, df, l.two);
+        store_pair<T, R>(row, ga + 2 * gs, dg, l.two);
       }
     }
-    if (a.dc0 && l.live && chunk == 0 && wave == 0) store_state<VEC>(a.dc0 + l.at, e, l.two);
+    if (a.dc0 && l.live && chunk == 0 && wave == 0) store_state<R>(a.dc0, l.at, e, l.two);
     if constexpr (LOOK) break;
   }
   if (!a.dbias) return;
@@ -567,7 +573,7 @@ __global__ void __launch_bounds__(256) linear_clear_kernel(u32x4* words, size_t 
 
 struct Plan {
   LinearScan s;
-  bool walk, look;
+  bool walk, look, fits;
   size_t lanes;          // pairs of units
   size_t maps, states, tickets, dpart;   // bytes
   int rows;              // of dpart
@@ -581,11 +587,20 @@ Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   p.s.cols = (int)((p.lanes + 63) / 64);
   p.s.chunks = std::max(1, (T + kChunk - 1) / kChunk);
   p.walk = !backward && T <= 16;
-  // (a grid has fewer than 2^32 threads)
-  p.look = !p.walk && p.s.chunks > 1 && p.s.cols < 2 * num_cu && (size_t)p.s.cols * p.s.chunks <= (1u << 22);
+  // Forward, chunks side by side where there are at least four and the columns
+  // alone leave compute units with fewer than two workgroups (bf16, H = 512, T = 512,
+  // side by side / one after another: 64 sequences 46 / 46 us, 128 89 / 78, 256 162 /
+  // 155; T = 100, H = 64, two chunks: 17 / 9.6 us, the words' clearing is a launch).
+  // Backward always: the loop needs more registers than there are (the same shapes
+  // forward and back: 126 / 126, 249 / 259, 460 / 510 us).  A grid has fewer than 2^32
+  // threads: beyond, forward takes the loop and backward is refused.
+  const size_t pieces = (size_t)p.s.cols * p.s.chunks;
+  p.look = !p.walk && p.s.chunks > 1 &&
+           (backward || (p.s.chunks >= 4 && p.s.cols < 2 * num_cu && pieces <= kMostChunks));
+  p.fits = !backward || pieces <= kMostChunks;
   if (p.look) {
     const size_t groups = (size_t)(p.s.chunks + kGroup - 1) / kGroup;
-    p.maps = (size_t)p.s.chunks * p.lanes * 16;
+    p.maps = ((size_t)p.s.chunks + p.s.chunks / kScanWaves) * p.lanes * 16;
     p.states = (groups * p.lanes * 8 + 15) / 16 * 16;
     p.tickets = (size_t)p.s.cols * kTicketStride * 4;
   }
@@ -607,36 +622,35 @@ hipError_t place(Plan& p, LinearArgs& a, void* ws, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Pairs of units may be read at once: H even, every array of pairs aligned to them.
-bool pairs_aligned(const LinearArgs& a) {
-  const size_t el = a.bf16 ? 2 : 4;
-  uintptr_t o = 0;
-  for (const void* p : {a.p, (const void*)a.h, a.dh, (const void*)a.dp}) o |= (uintptr_t)p % (2 * el);
-  for (const void* p : {(const void*)a.c0, (const void*)a.c_out, (const void*)a.c_save, (const void*)a.dc_out,
-                        (const void*)a.dc0})
-    o |= (uintptr_t)p % 8;
-  return a.H % 2 == 0 && o == 0;
-}
-
-template <class T, bool VEC>
+template <class T, Rows R>
 void launch_run(const LinearArgs& a, const Plan& p, hipStream_t stream) {
   if (p.walk)
-    linear_walk_kernel<T, VEC><<<(unsigned)((p.lanes + kWalkThreads - 1) / kWalkThreads), kWalkThreads, 0, stream>>>(a);
+    linear_walk_kernel<T, R><<<(unsigned)((p.lanes + kWalkThreads - 1) / kWalkThreads), kWalkThreads, 0, stream>>>(a);
   else if (p.look)
-    linear_scan_kernel<T, VEC, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+    linear_scan_kernel<T, R, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
   else
-    linear_scan_kernel<T, VEC, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
+    linear_scan_kernel<T, R, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
 }
 
-template <class T, bool VEC>
+template <class T, Rows R>
 void launch_back(const LinearArgs& a, const Plan& p, hipStream_t stream) {
   if (p.look)
-    linear_back_kernel<T, VEC, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+    linear_back_kernel<T, R, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
   else
-    linear_back_kernel<T, VEC, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
+    linear_back_kernel<T, R, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
+}
+
+// f of a's kind of rows
+template <class F>
+void rows_of(const LinearArgs& a, F f) {
+  if (a.H == 1) f(std::integral_constant<Rows, kSingle>{});
+  else if (a.H % 2) f(std::integral_constant<Rows, kOdd>{});
+  else f(std::integral_constant<Rows, kEven>{});
 }
 
 }  // namespace
+
+bool linear_fits(int T, int B, int H, int num_cu, int backward) { return plan_of(T, B, H, num_cu, backward).fits; }
 
 size_t linear_workspace(int T, int B, int H, int num_cu, int backward) {
   const Plan p = plan_of(T, B, H, num_cu, backward);
@@ -648,9 +662,8 @@ hipError_t launch_linear(const LinearArgs& a0, void* ws, hipStream_t stream) {
   Plan p = plan_of(a.T, a.B, a.H, a.num_cu, 0);
   const hipError_t e = place(p, a, ws, stream);
   if (e != hipSuccess) return e;
-  const bool vec = pairs_aligned(a);
-  if (a.bf16) vec ? launch_run<__bf16, true>(a, p, stream) : launch_run<__bf16, false>(a, p, stream);
-  else vec ? launch_run<float, true>(a, p, stream) : launch_run<float, false>(a, p, stream);
+  if (a.bf16) rows_of(a, [&](auto r) { launch_run<__bf16, decltype(r)::value>(a, p, stream); });
+  else rows_of(a, [&](auto r) { launch_run<float, decltype(r)::value>(a, p, stream); });
   return hipGetLastError();
 }
 
@@ -659,9 +672,8 @@ hipError_t launch_linear_backward(const LinearArgs& a0, void* ws, hipStream_t st
   Plan p = plan_of(a.T, a.B, a.H, a.num_cu, a.dbias ? 2 : 1);
   hipError_t e = place(p, a, ws, stream);
   if (e != hipSuccess) return e;
-  const bool vec = pairs_aligned(a);
-  if (a.bf16) vec ? launch_back<__bf16, true>(a, p, stream) : launch_back<__bf16, false>(a, p, stream);
-  else vec ? launch_back<float, true>(a, p, stream) : launch_back<float, false>(a, p, stream);
+  if (a.bf16) rows_of(a, [&](auto r) { launch_back<__bf16, decltype(r)::value>(a, p, stream); });
+  else rows_of(a, [&](auto r) { launch_back<float, decltype(r)::value>(a, p, stream); });
   e = hipGetLastError();
   if (e != hipSuccess || !a.dbias) return e;
   linear_dbias_kernel<<<(4 * a.H + 31) / 32, 1024, 0, stream>>>(a.dpart, p.rows, 4 * a.H, a.dbias);
