@@ -1814,8 +1814,8 @@ approx_lstm_status approx_lstm_q4_load(const uint8_t* q, const float* scale, con
   };
   step(hipGetDevice(&m->device), "hipGetDevice");
   if (st == APPROX_LSTM_OK) st = current_cus(&m->num_cu);
-  m->m.R = rows; m->m.D = cols; m->m.G = group; m->m.groups = (cols + group - 1) / group;
-  const size_t bytes = alstm::q4_bytes(rows, cols, group);
+  alstm::q4_shape(m->m, rows, cols, group);
+  const size_t bytes = alstm::q4_bytes(m->m);
   if (st == APPROX_LSTM_OK) step(hipMalloc(&m->d_store, bytes + 256), "hipMalloc(levels)");
   if (st == APPROX_LSTM_OK) {
     alstm::q4_place(m->m, m->d_store);

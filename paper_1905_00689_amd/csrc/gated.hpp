@@ -50,15 +50,20 @@ bool linear_fits(int T, int B, int H, int num_cu, int backward);
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_linear_backward(const LinearArgs& a, void* ws, hipStream_t stream);
 
-// A matrix of 4-bit levels (q4.hip).
+// A matrix of 4-bit levels: the store's layout is described in q4.hip.
 struct Q4Matrix {
-  uint8_t* q;         // [R][ceil(D/2)]
-  float* s;           // [R][groups]
-  float* z;           // [R][groups]
-  int R, D, G, groups;
+  unsigned* q;        // [tiles][blocks][64][4]
+  float* s;           // [tiles][padded][16]
+  uint8_t* z;         // [tiles][padded][16]
+  int R, D, G;
+  int groups;         // of a row: ceil(D / G)
+  int tiles;          // of 16 rows
+  int blocks;         // of 128 columns
+  int padded;         // groups of a padded row
 };
-// Bytes of device memory of a matrix, and its arrays' places there.
-size_t q4_bytes(int R, int D, int G);
+// Sizes of a matrix; its bytes of device memory; its arrays' places there.
+void q4_shape(Q4Matrix& m, int R, int D, int G);
+size_t q4_bytes(const Q4Matrix& m);
 void q4_place(Q4Matrix& m, uint8_t* store);
 // Lays out q [R][ceil(D/2)], scale [R][groups], zero [R][groups] (null: 8) in m;
 // *bad becomes 1 where a zero level is above 15.

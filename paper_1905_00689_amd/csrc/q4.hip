@@ -1,90 +1,388 @@
 // Products with a matrix of 4-bit levels on gfx950:
 //
 //   y[n][r] = bias[r] + sum_d s[r][d / G] (q[r][d] - z[r][d / G]) x[n][d].
+//
+// The levels enter v_mfma_f32_16x16x32_bf16 as whole numbers that bf16 holds
+// exactly, moved by a constant o that their bits make cheap, and the zero level
+// comes off with the group's sum of x:
+//
+//   y = bias + sum_g s (sum_d (q + o) x - (z + o) sum_d x),   sums and scales fp32.
+//
+// A = 16 rows of the matrix, B = 16 rows of x: lane l holds A[l%16][8 (l/16) .. +7],
+// B[8 (l/16) .. +7][l%16] and results of rows 4 (l/16) .. +3, column l%16.
+// bf16 x: o = 16, a level in the top bits of the mantissa of 16 .. 31 (two operations
+// a pair).  fp32 x: three bf16 parts of 8 bits each (exact), and o = -7.5, so that the
+// sums are not larger than they have to be.
+//
+// Store: [row tile of 16][block of 128 columns][lane][4 steps] words of eight levels:
+// a lane's weights of a block are one 16-byte load, a wave's 1 KB in a row.  In a
+// word, columns 0, 2, 4, 6 of the eight stand in the low half, 1, 3, 5, 7 in the high
+// one, which is where the pairs of a bf16 operand want them.  Rows and columns that
+// pad a tile hold level 0 and scale 0.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "gated.hpp"
+
+#pragma clang fp contract(off)
 
 namespace alstm {
 
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBlockCols = 128;
+
+__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// word of the store that holds level (r, d), and its bit
+struct Place {
+  size_t word;
+  int bit;
+};
+__device__ __forceinline__ Place place_of(const Q4Matrix& m, int r, int d) {
+  const int kb = d / kBlockCols, k = d % kBlockCols, step = k / 32, lane = (r & 15) + 16 * ((k & 31) / 8), e = k & 7;
+  return {(((size_t)(r >> 4) * m.blocks + kb) * 64 + lane) * 4 + step, 4 * (e / 2 + 4 * (e & 1))};
+}
+
 __global__ void __launch_bounds__(256) q4_layout_kernel(Q4Matrix m, const uint8_t* q, const float* scale,
                                                         const uint8_t* zero, int* bad) {
-  const size_t nq = (size_t)m.R * ((m.D + 1) / 2), ns = (size_t)m.R * m.groups;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < nq; i += (size_t)gridDim.x * 256) m.q[i] = q[i];
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < ns; i += (size_t)gridDim.x * 256) {
-    m.s[i] = scale[i];
-    const int z = zero ? zero[i] : 8;
-    m.z[i] = (float)z;
-    if (z > 15) *bad = 1;
+  const size_t row_bytes = ((size_t)m.D + 1) / 2, words = (size_t)m.tiles * m.blocks * 256;
+  const size_t first = (size_t)blockIdx.x * 256 + threadIdx.x, by = (size_t)gridDim.x * 256;
+  for (size_t i = first; i < words; i += by) {
+    const int step = (int)(i & 3), lane = (int)(i >> 2) & 63;
+    const size_t tile = (i >> 8) / m.blocks;
+    const int kb = (int)((i >> 8) % m.blocks);
+    const size_t r = tile * 16 + (lane & 15), d0 = (size_t)kb * kBlockCols + 32 * step + 8 * (lane >> 4);
+    unsigned w = 0;
+    for (int e = 0; e < 8; ++e)
+      if (r < (size_t)m.R && d0 + e < (size_t)m.D)
+        w |= (unsigned)((q[r * row_bytes + (d0 + e) / 2] >> (4 * (e & 1))) & 15) << (4 * (e / 2 + 4 * (e & 1)));
+    m.q[i] = w;
+  }
+  const size_t ns = (size_t)m.tiles * m.padded * 16;
+  for (size_t i = first; i < ns; i += by) {
+    const size_t r = i / 16 / m.padded * 16 + (i & 15);
+    const int g = (int)(i / 16 % m.padded);
+    float s = 0.f;
+    int z = 0;
+    if (r < (size_t)m.R && g < m.groups) {
+      s = scale[r * m.groups + g];
+      z = zero ? zero[r * m.groups + g] : 8;
+      if (z > 15) *bad = 1;
+    }
+    m.s[i] = s;
+    m.z[i] = (uint8_t)z;
   }
 }
 
 __global__ void __launch_bounds__(256) q4_unpack_kernel(Q4Matrix m, uint8_t* q, float* scale, uint8_t* zero) {
-  const size_t nq = (size_t)m.R * ((m.D + 1) / 2), ns = (size_t)m.R * m.groups;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < nq; i += (size_t)gridDim.x * 256) q[i] = m.q[i];
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < ns; i += (size_t)gridDim.x * 256) {
-    scale[i] = m.s[i];
-    zero[i] = (uint8_t)m.z[i];
+  const size_t row_bytes = ((size_t)m.D + 1) / 2, nq = (size_t)m.R * row_bytes, ns = (size_t)m.R * m.groups;
+  const size_t first = (size_t)blockIdx.x * 256 + threadIdx.x, by = (size_t)gridDim.x * 256;
+  for (size_t i = first; i < nq; i += by) {
+    const int r = (int)(i / row_bytes), d = 2 * (int)(i % row_bytes);
+    unsigned b = 0;
+    for (int e = 0; e < 2; ++e)
+      if (d + e < m.D) {
+        const Place p = place_of(m, r, d + e);
+        b |= ((m.q[p.word] >> p.bit) & 15u) << (4 * e);
+      }
+    q[i] = (uint8_t)b;
+  }
+  for (size_t i = first; i < ns; i += by) {
+    const size_t r = i / m.groups, at = ((r / 16) * m.padded + i % m.groups) * 16 + r % 16;
+    scale[i] = m.s[at];
+    zero[i] = m.z[at];
   }
 }
 
-// One wave per row and four rows of x: lane l takes every 64th column.
+// Eight levels of a word as bf16 16 + q.
+__device__ __forceinline__ bf16x8 levels_16(unsigned w) {
+  constexpr unsigned kMask = 0x00780078u, kOne = 0x41804180u;   // 16.0 in both halves
+  const u32x4 v{((w << 3) & kMask) | kOne, ((w >> 1) & kMask) | kOne, ((w >> 5) & kMask) | kOne,
+                ((w >> 9) & kMask) | kOne};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// Eight levels of a word as bf16 q - 7.5 = +-(m + 1/2), m = 0 .. 7: m picks the two
+// bytes of m + 1/2 from a table, bit 3 of the level is the sign.
+__device__ __forceinline__ bf16x8 levels_centred(unsigned w) {
+  const unsigned neg = ~w & 0x88888888u;        // levels below 8: m = 7 - q
+  w ^= neg - (neg >> 3);
+  const unsigned sign = neg;
+  constexpr unsigned kHi0 = 0x40403F3Fu, kHi1 = 0x40404040u, kLo0 = 0x6020C000u, kLo1 = 0xF0D0B090u;
+  // nibbles 0, 2, 4, 6 and 1, 3, 5, 7 of the word: columns 0, 4, 1, 5 and 2, 6, 3, 7
+  const unsigned ma = w & 0x07070707u, mb = (w >> 4) & 0x07070707u;
+  const unsigned ha = __builtin_amdgcn_perm(kHi1, kHi0, ma) | ((sign << 4) & 0x80808080u);
+  const unsigned hb = __builtin_amdgcn_perm(kHi1, kHi0, mb) | (sign & 0x80808080u);
+  const unsigned la = __builtin_amdgcn_perm(kLo1, kLo0, ma), lb = __builtin_amdgcn_perm(kLo1, kLo0, mb);
+  // byte i of ha, la: nibbles 0, 2, 4, 6 are columns 0, 4, 1, 5
+  const u32x4 v{__builtin_amdgcn_perm(ha, la, 0x06020400u), __builtin_amdgcn_perm(hb, lb, 0x06020400u),
+                __builtin_amdgcn_perm(ha, la, 0x07030501u), __builtin_amdgcn_perm(hb, lb, 0x07030501u)};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// Eight values of a row of x from column k, zeros past its end.
 template <class T>
-__global__ void __launch_bounds__(256) q4_row_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int n0 = blockIdx.y * 4;
-  if (r >= m.R) return;
-  const uint8_t* q = m.q + (size_t)r * ((m.D + 1) / 2);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int d = lane; d < m.D; d += 64) {
-    const size_t g = (size_t)r * m.groups + d / m.G;
-    const float w = m.s[g] * ((float)((q[d / 2] >> (4 * (d & 1))) & 15) - m.z[g]);
+struct XVec;
+template <>
+struct XVec<__bf16> {
+  typedef bf16x8 Raw;
+  typedef bf16x8 Any __attribute__((aligned(2)));
+};
+template <>
+struct XVec<float> {
+  typedef f32x8 Raw;
+  typedef f32x8 Any __attribute__((aligned(4)));
+};
+template <class T>
+__device__ __forceinline__ typename XVec<T>::Raw load_x(const T* row, int k, int D, bool whole) {
+  if (whole) return *reinterpret_cast<const typename XVec<T>::Any*>(row + k);
+  typename XVec<T>::Raw v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n0 + j < N) acc[j] = __builtin_fmaf(w, (float)x[(size_t)(n0 + j) * m.D + d], acc[j]);
+  for (int e = 0; e < 8; ++e) v[e] = k + e < D ? row[k + e] : (T)0.f;
+  return v;
+}
+
+// The bf16 parts of eight values: kParts of them, whose sum is the value.
+template <class T>
+struct Parts;
+template <>
+struct Parts<__bf16> {
+  static constexpr int kParts = 1;
+  static constexpr float kOffset = 16.f;
+  bf16x8 p[1];
+  __device__ __forceinline__ explicit Parts(const bf16x8& x) : p{x} {}
+  static __device__ __forceinline__ bf16x8 levels(unsigned w) { return levels_16(w); }
+};
+template <>
+struct Parts<float> {
+  static constexpr int kParts = 3;
+  static constexpr float kOffset = -7.5f;
+  bf16x8 p[3];
+  // cut, not rounded: the rest is exact, and the largest fp32 stays finite
+  __device__ __forceinline__ explicit Parts(const f32x8& x) {
+    u32x4 v[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned h[2], m[2], l[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float f = x[2 * i + j];
+        h[j] = __float_as_uint(f);
+        const float r = f - __uint_as_float(h[j] & 0xFFFF0000u);
+        m[j] = __float_as_uint(r);
+        l[j] = __float_as_uint(r - __uint_as_float(m[j] & 0xFFFF0000u));
+      }
+      v[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302u);
+      v[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302u);
+      v[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302u);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k] = __builtin_bit_cast(bf16x8, v[k]);
   }
+  static __device__ __forceinline__ bf16x8 levels(unsigned w) { return levels_centred(w); }
+};
+
+// scales and moved zero levels of four rows
+struct Scale {
+  f32x4 s, z;
+};
+template <class T>
+__device__ __forceinline__ Scale load_scale(const Q4Matrix& m, int tile, int g, int lg) {
+  const size_t at = ((size_t)tile * m.padded + g) * 16 + 4 * lg;
+  const unsigned z = *reinterpret_cast<const unsigned*>(m.z + at);
+  Scale v;
+  v.s = *reinterpret_cast<const f32x4*>(m.s + at);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float s = wave_sum(acc[j]);
-    if (lane == 0 && n0 + j < N) y[(size_t)(n0 + j) * m.R + r] = (T)(s + (bias ? bias[r] : 0.f));
+  for (int i = 0; i < 4; ++i) v.z[i] = (float)((z >> (8 * i)) & 255u) + Parts<T>::kOffset;
+  return v;
+}
+
+// y rows n, four columns from r
+template <class T>
+__device__ __forceinline__ void store_y(T* y, const float* bias, int R, size_t n, int r, f32x4 v) {
+  T* p = y + n * R + r;
+  if (r + 4 <= R) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    typedef Four Any __attribute__((aligned(sizeof(T))));
+    if (bias)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += bias[r + i];
+    *reinterpret_cast<Any*>(p) = __builtin_convertvector(v, Four);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r + i < R) p[i] = (T)(v[i] + (bias ? bias[r + i] : 0.f));
   }
 }
+
+// Few rows of x: what bounds it is reading the matrix, so every workgroup reads RT
+// row tiles of it once, its KW waves every KW-th block of columns, for up to 16 NT
+// rows of x straight from L2; the waves' sums meet in LDS, in order.
+template <class T, int G, int RT, int NT, int KW>
+__global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y) {
+  constexpr int kSteps = kBlockCols / 32, kGroupSteps = G / 32, kParts = Parts<T>::kParts;
+  __shared__ f32x4 part[KW][RT * NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  const int tile0 = blockIdx.x * RT, n0 = blockIdx.y * (16 * NT);
+  const T* row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) row[t] = x + (size_t)min(n0 + 16 * t + li, N - 1) * m.D;
+  f32x4 acc[RT][NT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+  u32x4 w[RT];
+  auto load_w = [&](int kb) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+      w[r] = *reinterpret_cast<const u32x4*>(
+          m.q + (((size_t)min(tile0 + r, m.tiles - 1) * m.blocks + kb) * 64 + lane) * 4);
+  };
+  if (wave < m.blocks) load_w(wave);
+  for (int kb = wave; kb < m.blocks; kb += KW) {
+    const int k0 = kb * kBlockCols + 8 * lg;
+    const bool whole = (kb + 1) * kBlockCols <= m.D;
+    typename XVec<T>::Raw xr[kSteps][NT];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xr[s][t] = load_x<T>(row[t], k0 + 32 * s, m.D, whole);
+    u32x4 now[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) now[r] = w[r];
+    if (kb + KW < m.blocks) load_w(kb + KW);
+    f32x4 p[RT][NT], sum[NT];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      if (s % kGroupSteps == 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int r = 0; r < RT; ++r) p[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      bf16x8 a[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) a[r] = Parts<T>::levels(now[r][s]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const Parts<T> b(xr[s][t]);
+#pragma unroll
+        for (int k = kParts - 1; k >= 0; --k) {   // the small parts first
+          sum[t] = mfma(ones, b.p[k], sum[t]);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) p[r][t] = mfma(a[r], b.p[k], p[r][t]);
+        }
+      }
+      if (s % kGroupSteps == kGroupSteps - 1) {
+        const int g = kb * (kBlockCols / G) + s / kGroupSteps;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const Scale c = load_scale<T>(m, min(tile0 + r, m.tiles - 1), g, lg);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[r][t][i] = __builtin_fmaf(c.s[i], __builtin_fmaf(-c.z[i], sum[t][i], p[r][t][i]), acc[r][t][i]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) part[wave][r * NT + t][lane] = acc[r][t];
+  __syncthreads();
+  for (int j = wave; j < RT * NT; j += KW) {
+    const int r = j / NT, t = j % NT, n = n0 + 16 * t + li, at = (tile0 + r) * 16 + 4 * lg;
+    f32x4 v = part[0][j][lane];
+#pragma unroll
+    for (int k = 1; k < KW; ++k) v += part[k][j][lane];
+    if (n < N && at < m.R) store_y<T>(y, bias, m.R, n, at, v);
+  }
+}
+
+template <class T, int G, int RT, int NT, int KW>
+void launch_rows(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, hipStream_t stream) {
+  const dim3 grid((m.tiles + RT - 1) / RT, (N + 16 * NT - 1) / (16 * NT));
+  q4_rows_kernel<T, G, RT, NT, KW><<<grid, 64 * KW, 0, stream>>>(m, x, N, bias, y);
+}
+
+template <class T, int G>
+void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, int num_cu, hipStream_t stream) {
+  (void)num_cu;
+  if (N <= 16) {
+    if (m.tiles >= 1024) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
+    else launch_rows<T, G, 1, 1, 8>(m, x, N, bias, y, stream);
+  } else {
+    launch_rows<T, G, 2, 4, 8>(m, x, N, bias, y, stream);
+  }
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t q4_bytes(int R, int D, int G) {
-  const size_t groups = (size_t)(D + G - 1) / G;
-  return ((size_t)R * ((D + 1) / 2) + 255) / 256 * 256 + 2 * (((size_t)R * groups * 4 + 255) / 256 * 256);
+void q4_shape(Q4Matrix& m, int R, int D, int G) {
+  m.R = R, m.D = D, m.G = G;
+  m.groups = (D + G - 1) / G;
+  m.tiles = (R + 15) / 16;
+  m.blocks = (D + kBlockCols - 1) / kBlockCols;
+  m.padded = m.blocks * (kBlockCols / G);
+}
+
+size_t q4_bytes(const Q4Matrix& m) {
+  const size_t scales = (size_t)m.tiles * m.padded * 16;
+  return (size_t)m.tiles * m.blocks * 1024 + up256(scales * 4) + up256(scales);
 }
 
 void q4_place(Q4Matrix& m, uint8_t* store) {
-  m.q = store;
-  store += ((size_t)m.R * ((m.D + 1) / 2) + 255) / 256 * 256;
+  const size_t scales = (size_t)m.tiles * m.padded * 16;
+  m.q = reinterpret_cast<unsigned*>(store);
+  store += (size_t)m.tiles * m.blocks * 1024;
   m.s = reinterpret_cast<float*>(store);
-  store += ((size_t)m.R * m.groups * 4 + 255) / 256 * 256;
-  m.z = reinterpret_cast<float*>(store);
+  m.z = store + up256(scales * 4);
 }
 
 hipError_t launch_q4_layout(const Q4Matrix& m, const uint8_t* q, const float* scale, const uint8_t* zero, int* bad,
                             hipStream_t stream) {
-  q4_layout_kernel<<<1024, 256, 0, stream>>>(m, q, scale, zero, bad);
+  q4_layout_kernel<<<2048, 256, 0, stream>>>(m, q, scale, zero, bad);
   return hipGetLastError();
 }
 
 hipError_t launch_q4_unpack(const Q4Matrix& m, uint8_t* q, float* scale, uint8_t* zero, hipStream_t stream) {
-  q4_unpack_kernel<<<1024, 256, 0, stream>>>(m, q, scale, zero);
+  q4_unpack_kernel<<<2048, 256, 0, stream>>>(m, q, scale, zero);
   return hipGetLastError();
 }
 
 hipError_t launch_q4(const Q4Matrix& m, const void* x, int N, int bf16, const float* bias, void* y, int num_cu,
                      hipStream_t stream) {
-  (void)num_cu;
-  const dim3 grid((m.R + 3) / 4, (N + 3) / 4);
-  if (bf16) q4_row_kernel<__bf16><<<grid, 256, 0, stream>>>(m, (const __bf16*)x, N, bias, (__bf16*)y);
-  else q4_row_kernel<float><<<grid, 256, 0, stream>>>(m, (const float*)x, N, bias, (float*)y);
+  constexpr int kMostRows = 1 << 20;   // of a launch (a grid's second dimension is short)
+  auto go = [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    for (int n = 0; n < N; n += std::min(N - n, kMostRows)) {
+      const int c = std::min(N - n, kMostRows);
+      const size_t in = (size_t)n * m.D, out = (size_t)n * m.R;
+      if (bf16) launch_group<__bf16, G>(m, (const __bf16*)x + in, c, bias, (__bf16*)y + out, num_cu, stream);
+      else launch_group<float, G>(m, (const float*)x + in, c, bias, (float*)y + out, num_cu, stream);
+    }
+  };
+  if (m.G == 32) go(std::integral_constant<int, 32>{});
+  else if (m.G == 64) go(std::integral_constant<int, 64>{});
+  else go(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 
