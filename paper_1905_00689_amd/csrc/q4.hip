@@ -129,7 +129,8 @@ __device__ __forceinline__ bf16x8 levels_centred(unsigned w) {
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Eight values of a row of x from column k, zeros past its end.
+// Eight values of a row of x from column k, zeros past its end; `whole`: none is.
+// (Loads of these types need be aligned to their elements only.)
 template <class T>
 struct XVec;
 template <>
@@ -145,9 +146,16 @@ struct XVec<float> {
 template <class T>
 __device__ __forceinline__ typename XVec<T>::Raw load_x(const T* row, int k, int D, bool whole) {
   if (whole) return *reinterpret_cast<const typename XVec<T>::Any*>(row + k);
-  typename XVec<T>::Raw v;
+  typename XVec<T>::Raw v{};
+  if (k + 8 <= D) {
+    v = *reinterpret_cast<const typename XVec<T>::Any*>(row + k);
+  } else if (k < D) {   // (eight loads at once, not one after another)
+    T t[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = k + e < D ? row[k + e] : (T)0.f;
+    for (int e = 0; e < 8; ++e) t[e] = row[min(k + e, D - 1)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k + e < D ? t[e] : (T)0.f;
+  }
   return v;
 }
 
@@ -190,6 +198,12 @@ struct Parts<float> {
   }
   static __device__ __forceinline__ bf16x8 levels(unsigned w) { return levels_centred(w); }
 };
+
+// the sum of eight values
+__device__ __forceinline__ float sum8(const f32x8& v) {
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+__device__ __forceinline__ float sum8(const bf16x8& v) { return sum8(__builtin_convertvector(v, f32x8)); }
 
 // scales and moved zero levels of four rows
 struct Scale {
@@ -243,7 +257,7 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-  u32x4 w[RT];
+  u32x4 w[RT];   // the next block's, under way while a block is multiplied
   auto load_w = [&](int kb) {
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -252,13 +266,12 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
   };
   if (wave < m.blocks) load_w(wave);
   for (int kb = wave; kb < m.blocks; kb += KW) {
-    const int k0 = kb * kBlockCols + 8 * lg;
     const bool whole = (kb + 1) * kBlockCols <= m.D;
     typename XVec<T>::Raw xr[kSteps][NT];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) xr[s][t] = load_x<T>(row[t], k0 + 32 * s, m.D, whole);
+      for (int t = 0; t < NT; ++t) xr[s][t] = load_x<T>(row[t], kb * kBlockCols + 8 * lg + 32 * s, m.D, whole);
     u32x4 now[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) now[r] = w[r];
@@ -315,21 +328,259 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
   }
 }
 
+// One or two rows of x in fp32: with 14 of 16 columns of an operand idle, splitting x
+// and centring the levels costs more than multiplying on the vector units.  A lane
+// has the row of the matrix and the columns that its words hold; its products begin
+// at -z sum x, so that they end up no larger than they have to be.
+template <class T, int G, int RT, int NX, int KW>
+__global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y) {
+  constexpr int kSteps = kBlockCols / 32, kGroupSteps = G / 32, kGroups = kBlockCols / G;
+  __shared__ float part[KW][RT * NX][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lg = lane >> 4, tile0 = blockIdx.x * RT;
+  float acc[RT][NX] = {};
+  const unsigned* wp[RT];
+  size_t at_scale[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const size_t tile = (size_t)min(tile0 + r, m.tiles - 1);
+    wp[r] = m.q + (tile * m.blocks * 64 + lane) * 4;
+    at_scale[r] = tile * m.padded * 16 + li;
+  }
+  u32x4 w[RT];
+  float s[RT][kGroups];
+  unsigned z[RT][kGroups];
+  auto load = [&](int kb) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      w[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wp[r] + (size_t)kb * 256));
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        s[r][g] = m.s[at_scale[r] + (size_t)(kb * kGroups + g) * 16];
+        z[r][g] = m.z[at_scale[r] + (size_t)(kb * kGroups + g) * 16];
+      }
+    }
+  };
+  for (int kb = wave; kb < m.blocks; kb += KW) {
+    load(kb);
+    const int k0 = kb * kBlockCols + 8 * lg;
+    const bool whole = (kb + 1) * kBlockCols <= m.D;
+    f32x8 xv[kSteps][NX];
+    float sum[kSteps][NX];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int n = 0; n < NX; ++n) {
+        xv[k][n] = __builtin_convertvector(load_x<T>(x + (size_t)min(n, N - 1) * m.D, k0 + 32 * k, m.D, whole), f32x8);
+        sum[k][n] = sum8(xv[k][n]);
+      }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        float t[NX] = {};
+        const float zf = -(float)z[r][g];
+#pragma unroll
+        for (int j = 0; j < kGroupSteps; ++j) {
+          const int k = g * kGroupSteps + j;
+          const unsigned a = w[r][k] & 0x0F0F0F0Fu, b = (w[r][k] >> 4) & 0x0F0F0F0Fu;
+          // bytes of a: columns 0, 4, 1, 5; of b: 2, 6, 3, 7
+          const float q[8] = {(float)(a & 255u), (float)((a >> 16) & 255u), (float)(b & 255u), (float)((b >> 16) & 255u),
+                              (float)((a >> 8) & 255u), (float)(a >> 24), (float)((b >> 8) & 255u), (float)(b >> 24)};
+#pragma unroll
+          for (int n = 0; n < NX; ++n) {
+            t[n] = __builtin_fmaf(zf, sum[k][n], t[n]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[n] = __builtin_fmaf(q[e], xv[k][n][e], t[n]);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NX; ++n) acc[r][n] = __builtin_fmaf(s[r][g], t[n], acc[r][n]);
+      }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int n = 0; n < NX; ++n) part[wave][r * NX + n][lane] = acc[r][n];
+  __syncthreads();
+  for (int j = threadIdx.x; j < 16 * RT * NX; j += 64 * KW) {
+    const int i = j & 15, r = (j >> 4) / NX, n = (j >> 4) % NX, at = (tile0 + r) * 16 + i;
+    if (n >= N || at >= m.R) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) v += part[k][j >> 4][16 * g + i];
+    y[(size_t)n * m.R + at] = (T)(v + (bias ? bias[at] : 0.f));
+  }
+}
+
+// Many rows of x: a matrix product.  A workgroup takes 256 rows of the matrix and 64
+// of x; its four waves 64 rows each, whose levels go from the store to operands
+// without LDS (nobody else needs them), while x, which all four need, is staged
+// there a block of columns at a time, the next block's loads under way meanwhile.  The
+// group sums of x are formed by the threads that stage it.
+constexpr int kTileRows = 256, kTileThreads = 256;
+constexpr int kTileLd = kBlockCols + 8;   // LDS row (bf16): 16-byte reads of 16 rows in distinct banks
+
+template <class T, int G, int X>
+struct TileLds {
+  alignas(16) uint16_t x[Parts<T>::kParts][X][kTileLd];
+  alignas(16) float s[kBlockCols / G][kTileRows];   // scales and moved zero levels of the rows
+  alignas(16) float z[kBlockCols / G][kTileRows];
+  float sum[kBlockCols / G][X];                     // group sums of x
+};
+
+template <class T, int G, int NT>
+__global__ void __launch_bounds__(kTileThreads, NT == 4 ? 2 : 3) q4_tile_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y,
+                                                               int row_blocks, int x_blocks) {
+  constexpr int RT = 4, kTileX = 16 * NT, kSteps = kBlockCols / 32, kGroupSteps = G / 32, kGroups = kBlockCols / G,
+                kParts = Parts<T>::kParts, kChunks = kTileX * kBlockCols / 8 / kTileThreads;
+  constexpr int kBuffers = kParts == 1 ? 2 : 1;   // (two of fp32's would leave room for one workgroup)
+  __shared__ TileLds<T, G, kTileX> lds[kBuffers];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  // consecutive workgroups go to the 8 XCDs in turn: an XCD takes whole blocks of x
+  const int b = blockIdx.x, xb = (b % 8) + 8 * (b / (8 * row_blocks)), rb = (b / 8) % row_blocks;
+  if (xb >= x_blocks) return;
+  const int tile0 = rb * (kTileRows / 16) + wave * RT, n0 = xb * kTileX;
+  const T* row[kChunks];
+  int col[kChunks];
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    const int i = tid + kTileThreads * j;
+    row[j] = x + (size_t)min(n0 + i / 16, N - 1) * m.D;
+    col[j] = (i % 16) * 8;
+  }
+  const unsigned* wp[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) wp[r] = m.q + ((size_t)min(tile0 + r, m.tiles - 1) * m.blocks * 64 + lane) * 4;
+  const size_t at_scale = (size_t)min(rb * (kTileRows / 16) + tid / 16, m.tiles - 1) * m.padded * 16 + (tid & 15);
+  typename XVec<T>::Raw xr[kChunks];
+  u32x4 w[RT];
+  float rs[kGroups];
+  unsigned rz[kGroups];
+  auto load = [&](int kb) {
+    const bool whole = (kb + 1) * kBlockCols <= m.D;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) xr[j] = load_x<T>(row[j], kb * kBlockCols + col[j], m.D, whole);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) w[r] = *reinterpret_cast<const u32x4*>(wp[r] + (size_t)kb * 256);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      rs[g] = m.s[at_scale + (size_t)(kb * kGroups + g) * 16];
+      rz[g] = m.z[at_scale + (size_t)(kb * kGroups + g) * 16];
+    }
+  };
+  f32x4 acc[RT][NT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load(0);
+  for (int kb = 0; kb < m.blocks; ++kb) {
+    TileLds<T, G, kTileX>& l = lds[kb % kBuffers];
+    if (kBuffers == 1) lds_barrier();
+    u32x4 now[RT];
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      const int i = tid + kTileThreads * j;
+      const Parts<T> v(xr[j]);
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) *reinterpret_cast<bf16x8*>(&l.x[k][i / 16][(i % 16) * 8]) = v.p[k];
+      const float s = group_sum<G / 8>(sum8(xr[j]));
+      if (i % (G / 8) == 0) l.sum[(i % 16) / (G / 8)][i / 16] = s;
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      l.s[g][tid] = rs[g];
+      l.z[g][tid] = (float)rz[g] + Parts<T>::kOffset;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) now[r] = w[r];
+    lds_barrier();
+    if (kb + 1 < m.blocks) load(kb + 1);
+    f32x4 p[RT][NT];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      if (s % kGroupSteps == 0) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) p[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      bf16x8 a[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) a[r] = Parts<T>::levels(now[r][s]);
+#pragma unroll
+      for (int k = kParts - 1; k >= 0; --k)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const bf16x8 v = *reinterpret_cast<const bf16x8*>(&l.x[k][16 * t + li][32 * s + 8 * lg]);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) p[r][t] = mfma(a[r], v, p[r][t]);
+        }
+      if (s % kGroupSteps == kGroupSteps - 1) {
+        const int g = s / kGroupSteps;
+        float sum[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[t] = l.sum[g][16 * t + li];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const f32x4 cs = *reinterpret_cast<const f32x4*>(&l.s[g][64 * wave + 16 * r + 4 * lg]);
+          const f32x4 cz = *reinterpret_cast<const f32x4*>(&l.z[g][64 * wave + 16 * r + 4 * lg]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[r][t][i] = __builtin_fmaf(cs[i], __builtin_fmaf(-cz[i], sum[t], p[r][t][i]), acc[r][t][i]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int n = n0 + 16 * t + li, at = (tile0 + r) * 16 + 4 * lg;
+      if (n < N && at < m.R) store_y<T>(y, bias, m.R, n, at, acc[r][t]);
+    }
+}
+
+template <class T, int G, int NT>
+void launch_tile(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, hipStream_t stream) {
+  const int rb = (m.R + kTileRows - 1) / kTileRows, xb = (N + 16 * NT - 1) / (16 * NT);
+  q4_tile_kernel<T, G, NT><<<(unsigned)((xb + 7) / 8 * 8 * rb), kTileThreads, 0, stream>>>(m, x, N, bias, y, rb, xb);
+}
+
 template <class T, int G, int RT, int NT, int KW>
 void launch_rows(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, hipStream_t stream) {
   const dim3 grid((m.tiles + RT - 1) / RT, (N + 16 * NT - 1) / (16 * NT));
   q4_rows_kernel<T, G, RT, NT, KW><<<grid, 64 * KW, 0, stream>>>(m, x, N, bias, y);
 }
 
+template <class T, int G, int RT, int NX, int KW>
+void launch_dot(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, hipStream_t stream) {
+  q4_dot_kernel<T, G, RT, NX, KW><<<(m.tiles + RT - 1) / RT, 64 * KW, 0, stream>>>(m, x, N, bias, y);
+}
+
 template <class T, int G>
 void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, int num_cu, hipStream_t stream) {
-  (void)num_cu;
-  if (N <= 16) {
-    if (m.tiles >= 1024) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
-    else launch_rows<T, G, 1, 1, 8>(m, x, N, bias, y, stream);
-  } else {
-    launch_rows<T, G, 2, 4, 8>(m, x, N, bias, y, stream);
-  }
+  // the tile kernel from a workgroup per compute unit on; below, the widest shape of
+  // the row kernel that still has one
+  const size_t tiles = m.tiles, cu = num_cu;
+  auto cover = [](size_t n, size_t by) { return (n + by - 1) / by; };
+  if (N > 64 && cover(m.R, kTileRows) * cover(N, 64) >= 2 * cu) launch_tile<T, G, 4>(m, x, N, bias, y, stream);
+  else if (N > 64 && cover(m.R, kTileRows) * cover(N, 32) >= (sizeof(T) == 2 ? cu / 2 + 1 : cu)) launch_tile<T, G, 2>(m, x, N, bias, y, stream);
+  else if (N == 1 && tiles >= 4 * cu) launch_dot<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
+  else if (N == 1 && tiles >= 2 * cu) launch_dot<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
+  else if (N == 1) launch_dot<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
+  else if (N == 2 && sizeof(T) == 4 && tiles >= 2 * cu) launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+  else if (N == 2 && sizeof(T) == 4) launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
+  else if (N <= 16 && tiles >= 4 * cu) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
+  else if (N > 32 && cover(tiles, 2) * cover(N, 64) >= cu) launch_rows<T, G, 2, 4, 8>(m, x, N, bias, y, stream);
+  else if (N > 16 && cover(tiles, 2) * cover(N, 32) >= cu) launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+  else launch_rows<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }

@@ -43,7 +43,8 @@ def check(y, q, s, z, G, x, bias):
 
 SHAPES = [(1, 1, 1, 32), (1, 128, 64, 128), (1, 100, 77, 32), (2, 16, 128, 64), (3, 33, 129, 128), (5, 256, 2048, 128),
           (16, 48, 260, 32), (17, 64, 96, 64), (31, 129, 500, 128), (48, 300, 257, 64), (64, 20, 1000, 32),
-          (65, 512, 64, 32), (100, 256, 1030, 32), (129, 130, 127, 64), (300, 272, 520, 128), (700, 96, 40, 32)]
+          (65, 512, 64, 32), (100, 256, 1030, 32), (129, 130, 127, 64), (300, 272, 520, 128), (700, 96, 40, 32),
+          (1100, 4000, 200, 32), (2050, 2100, 300, 128), (4200, 1000, 129, 64), (70, 33000, 64, 32)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
