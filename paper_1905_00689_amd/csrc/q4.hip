@@ -32,7 +32,7 @@ namespace alstm {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
@@ -105,7 +105,9 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(Q4Matrix m, uint8_t* q, 
 
 // Eight levels of a word as bf16 16 + q.
 __device__ __forceinline__ bf16x8 levels_16(unsigned w) {
-  constexpr unsigned kMask = 0x00780078u, kOne = 0x41804180u;   // 16.0 in both halves
+  constexpr unsigned kMask = 0x00780078u;
+  unsigned kOne = 0x41804180u;   // 16.0 in both halves
+  asm("" : "+v"(kOne));          // (in a vector register: one instruction masks and sets, and it takes one constant)
   const u32x4 v{((w << 3) & kMask) | kOne, ((w >> 1) & kMask) | kOne, ((w >> 5) & kMask) | kOne,
                 ((w >> 9) & kMask) | kOne};
   return __builtin_bit_cast(bf16x8, v);
@@ -203,7 +205,14 @@ struct Parts<float> {
 __device__ __forceinline__ float sum8(const f32x8& v) {
   return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
-__device__ __forceinline__ float sum8(const bf16x8& v) { return sum8(__builtin_convertvector(v, f32x8)); }
+__device__ __forceinline__ float sum8(const bf16x8& v) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), one, s, false);
+  return s;
+}
 
 // scales and moved zero levels of four rows
 struct Scale {
