@@ -271,10 +271,11 @@ __device__ __forceinline__ f32x4 await_map(const unsigned long long* w) {
                __uint_as_float((unsigned)(v[1] >> 32)), __uint_as_float((unsigned)v[1])};
 }
 
+template <int W>
 struct ScanLds {
-  f32x4 wave[2][kScanWaves][64];   // maps of the waves (of even and odd rounds)
-  f32x4 chunks[kScanWaves][64];    // maps of the chunks before in the block
-  f32x4 blocks[kScanWaves][64];    // maps of the blocks before in the group
+  f32x4 wave[2][W][64];            // maps of the waves (of even and odd rounds)
+  f32x4 chunks[W][64];             // maps of the chunks before in the block
+  f32x4 blocks[W][64];             // maps of the blocks before in the group
   f32x4 total[64];                 // map of the chunk
   f32x2 entry[64];                 // the state that the chunk begins with
   int ticket;
@@ -286,7 +287,7 @@ struct ScanLds {
 // read by the first chunk alone, which hands it on too, since the last chunk's
 // state may be written to the same place.
 template <class Load>
-__device__ __forceinline__ f32x2 hand_over(ScanLds& lds, const LinearScan& s, int order, int wave_order, int lane,
+__device__ __forceinline__ f32x2 hand_over(ScanLds<kScanWaves>& lds, const LinearScan& s, int order, int wave_order, int lane,
                                            size_t idx, bool live, Load first) {
   const int block = order / kScanWaves, i = order % kScanWaves, group = block / kScanWaves, j = block % kScanWaves;
   const bool last = order + 1 >= s.chunks;
@@ -337,7 +338,7 @@ __device__ __forceinline__ f32x2 hand_over(ScanLds& lds, const LinearScan& s, in
 // column's chunks one after another and keeps the state.
 template <class T, Rows R, bool LOOK>
 __global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T) == 4) ? 6 : 4) linear_scan_kernel(LinearArgs a, LinearScan s) {
-  __shared__ ScanLds lds;
+  __shared__ ScanLds<kScanWaves> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int col = blockIdx.x, chunk = 0;
   if constexpr (LOOK) {
@@ -360,25 +361,26 @@ __global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T)
     const int t0 = chunk * kChunk + wave * kSteps;
     const int n = min(l.len - t0, kSteps);   // timesteps here that the sequence has
     const bool some = __any(n > 0);          // (a wave of padding alone loads nothing)
-    typename Pair<T>::Raw raw[kSteps][4] = {};
-    if (some)
+    typename Pair<T>::Raw raw[kSteps][4];
+    f32x2 f[kSteps], u[kSteps];
+    if (some) {
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
         const char* row = (const char*)a.p + (size_t)min(t0 + k, a.T - 1) * (4 * BH * sizeof(T));
 #pragma unroll
         for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, R>(row, ga + q * gs, l.two);
       }
-    f32x2 f[kSteps], u[kSteps];
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]);
+      for (int k = 0; k < kSteps; ++k) {
+        const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        f[k][j] = gate_forget(yf[j], bias.f[j]);
-        u[k][j] = gate_sig(yi[j], bias.i[j]) * gate_tanh(yg[j], bias.g[j]);
+        for (int j = 0; j < 2; ++j) {
+          f[k][j] = gate_forget(yf[j], bias.f[j]);
+          u[k][j] = gate_sig(yi[j], bias.i[j]) * gate_tanh(yg[j], bias.g[j]);
+        }
       }
     }
-    if (a.lengths || t0 + kSteps > a.T) {
+    if (!some || a.lengths || t0 + kSteps > a.T) {
 #pragma unroll
       for (int k = 0; k < kSteps; ++k)
         if (k >= n) f[k] = f32x2{1.f, 1.f}, u[k] = f32x2{0.f, 0.f};
@@ -428,9 +430,12 @@ __global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T)
 // A wave runs its 8 steps forward from the saved state, so c is neither stored nor
 // read but every 8 timesteps, and keeps f, w and the three factors of d; its map is
 // e -> A e + B again.  The sums of dp over its timesteps leave through dpart.
-template <class T, Rows R, bool LOOK>
-__global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs a, LinearScan s) {
-  __shared__ ScanLds lds;
+// LOOK: a workgroup takes one of its column's chunks; else there is one.  W waves: 8,
+// or 2 for up to 16 timesteps.
+template <class T, Rows R, bool LOOK, int W>
+__global__ void __launch_bounds__(64 * W, 4) linear_back_kernel(LinearArgs a, LinearScan s) {
+  static_assert(!LOOK || W == kScanWaves, "chunks that hand over have eight waves");
+  __shared__ ScanLds<W> lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int col = blockIdx.x, order = 0;
   if constexpr (LOOK) {
@@ -446,14 +451,15 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
   const GateBias bias = gate_bias(a, l);
   const size_t BH = (size_t)a.B * a.H;
   const unsigned ga = (4u * l.b * a.H + l.r) * sizeof(T), gs = (unsigned)a.H * sizeof(T), ha = l.at * sizeof(T);
-  const int place = kScanWaves - 1 - wave;   // the wave's place in the order of the pass
+  const int place = W - 1 - wave;   // the wave's place in the order of the pass
   auto first = [&] { return a.dc_out ? load_state<R>(a.dc_out, l.at, l.two) : f32x2{0.f, 0.f}; };
   if (!LOOK && place == 0) lds.entry[lane] = first();   // (one wave reads it: dc0 may be dc_out)
-  f32x2 carry{0.f, 0.f};
   f32x2 si{0.f, 0.f}, sf = si, sg = si, so = si;
-  for (; order < s.chunks; ++order) {
-    const int chunk = s.chunks - 1 - order, t0 = chunk * kChunk + wave * kSteps;
-    typename Pair<T>::Raw raw[kSteps][4], rdh[kSteps];
+  const int chunk = s.chunks - 1 - order, t0 = chunk * (kSteps * W) + wave * kSteps;
+  const int n = min(l.len - t0, kSteps);
+  const bool some = __any(n > 0);
+  typename Pair<T>::Raw raw[kSteps][4] = {}, rdh[kSteps] = {};
+  if (some)
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
       const size_t t = (size_t)min(t0 + k, a.T - 1);
@@ -462,72 +468,62 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
       for (int q = 0; q < 4; ++q) raw[k][q] = load_pair<T, R>(row, ga + q * gs, l.two);
       rdh[k] = load_pair<T, R>((const char*)a.dh + t * (BH * sizeof(T)), ha, l.two);
     }
-    f32x2 c = load_state<R>(a.c_save + (size_t)(min(t0, a.T - 1) / kSteps) * BH, l.at, l.two);
-    const int n = min(l.len - t0, kSteps);
-    f32x2 f[kSteps], w[kSteps], ki[kSteps], kf[kSteps], kg[kSteps];
+  f32x2 c = load_state<R>(a.c_save + (size_t)(min(t0, a.T - 1) / kSteps) * BH, l.at, l.two);
+  f32x2 f[kSteps], w[kSteps], ki[kSteps], kf[kSteps], kg[kSteps];
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]),
-                  yo = Pair<T>::get(raw[k][3]), dh = Pair<T>::get(rdh[k]);
-      f32x2 dO;
+  for (int k = 0; k < kSteps; ++k) {
+    const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]),
+                yo = Pair<T>::get(raw[k][3]), dh = Pair<T>::get(rdh[k]);
+    f32x2 dO;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float vf = gate_forget(yf[j], bias.f[j]), vi = gate_sig(yi[j], bias.i[j]), vg = gate_tanh(yg[j], bias.g[j]),
-                    vo = gate_sig(yo[j], bias.o[j]);
-        kf[k][j] = c[j] * __builtin_fmaf(-vf, vf, vf);
-        ki[k][j] = vg * __builtin_fmaf(-vi, vi, vi);
-        kg[k][j] = vi * __builtin_fmaf(-vg, vg, 1.f);
-        const float cn = __builtin_fmaf(vf, c[j], vi * vg), tc = gate_tanh(cn, 0.f), dho = dh[j] * vo;
-        f[k][j] = vf;
-        w[k][j] = dho * __builtin_fmaf(-tc, tc, 1.f);
-        dO[j] = dho * tc * (1.f - vo);
-        if (k >= n) f[k][j] = 1.f, w[k][j] = kf[k][j] = ki[k][j] = kg[k][j] = dO[j] = 0.f;
-        else c[j] = cn;
-        so[j] += dO[j];
-      }
-      if (l.live && t0 + k < a.T)
-        store_pair<T, R>((char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T)), ga + 3 * gs, dO, l.two);
+    for (int j = 0; j < 2; ++j) {
+      const float vf = gate_forget(yf[j], bias.f[j]), vi = gate_sig(yi[j], bias.i[j]), vg = gate_tanh(yg[j], bias.g[j]),
+                  vo = gate_sig(yo[j], bias.o[j]);
+      kf[k][j] = c[j] * __builtin_fmaf(-vf, vf, vf);
+      ki[k][j] = vg * __builtin_fmaf(-vi, vi, vi);
+      kg[k][j] = vi * __builtin_fmaf(-vg, vg, 1.f);
+      const float cn = __builtin_fmaf(vf, c[j], vi * vg), tc = gate_tanh(cn, 0.f), dho = dh[j] * vo;
+      f[k][j] = vf;
+      w[k][j] = dho * __builtin_fmaf(-tc, tc, 1.f);
+      dO[j] = dho * tc * (1.f - vo);
+      if (k >= n) f[k][j] = 1.f, w[k][j] = kf[k][j] = ki[k][j] = kg[k][j] = dO[j] = 0.f;
+      else c[j] = cn;
+      so[j] += dO[j];
     }
-    f32x4 m = kIdentity;
-#pragma unroll
-    for (int k = kSteps - 1; k >= 0; --k)
-      m = then(m, f32x4{f[k][0], f[k][0] * w[k][0], f[k][1], f[k][1] * w[k][1]});
-    const int half = LOOK ? 0 : order & 1;
-    lds.wave[half][place][lane] = m;
-    lds_barrier();
-    f32x2 e = !LOOK && order == 0 ? lds.entry[lane] : carry;
-    if constexpr (LOOK) e = hand_over(lds, s, order, place, lane, idx, l.live, first);
-#pragma unroll 2
-    for (int v = 0; v < kScanWaves; ++v) {
-      if (v == place) carry = e;
-      if (LOOK && v == place) break;
-      e = apply(lds.wave[half][v][lane], e);
-    }
-    f32x2 next = e;
-    e = carry;
-    carry = next;
-#pragma unroll
-    for (int k = kSteps - 1; k >= 0; --k) {
-      f32x2 di, df, dg;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float d = w[k][j] + e[j];
-        di[j] = d * ki[k][j], df[j] = d * kf[k][j], dg[j] = d * kg[k][j];
-        e[j] = f[k][j] * d;
-        si[j] += di[j], sf[j] += df[j], sg[j] += dg[j];
-      }
-      if (l.live && t0 + k < a.T) {
-        char* row = (char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T));
-        store_pair<T, R>(row, ga, di, l.two);
-        store_pair<T, R>(row, ga + gs, df, l.two);
-        store_pair<T, R>(row, ga + 2 * gs, dg, l.two);
-      }
-    }
-    if (a.dc0 && l.live && chunk == 0 && wave == 0) store_state<R>(a.dc0, l.at, e, l.two);
-    if constexpr (LOOK) break;
+    if (l.live && t0 + k < a.T)
+      store_pair<T, R>((char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T)), ga + 3 * gs, dO, l.two);
   }
+  f32x4 m = kIdentity;
+#pragma unroll
+  for (int k = kSteps - 1; k >= 0; --k)
+    m = then(m, f32x4{f[k][0], f[k][0] * w[k][0], f[k][1], f[k][1] * w[k][1]});
+  lds.wave[0][place][lane] = m;
+  lds_barrier();
+  f32x2 e;
+  if constexpr (LOOK) e = hand_over(lds, s, order, place, lane, idx, l.live, first);
+  else e = lds.entry[lane];
+#pragma unroll 1
+  for (int v = 0; v < place; ++v) e = apply(lds.wave[0][v][lane], e);
+#pragma unroll
+  for (int k = kSteps - 1; k >= 0; --k) {
+    f32x2 di, df, dg;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float d = w[k][j] + e[j];
+      di[j] = d * ki[k][j], df[j] = d * kf[k][j], dg[j] = d * kg[k][j];
+      e[j] = f[k][j] * d;
+      si[j] += di[j], sf[j] += df[j], sg[j] += dg[j];
+    }
+    if (l.live && t0 + k < a.T) {
+      char* row = (char*)a.dp + (size_t)(t0 + k) * (4 * BH * sizeof(T));
+      store_pair<T, R>(row, ga, di, l.two);
+      store_pair<T, R>(row, ga + gs, df, l.two);
+      store_pair<T, R>(row, ga + 2 * gs, dg, l.two);
+    }
+  }
+  if (a.dc0 && l.live && chunk == 0 && wave == 0) store_state<R>(a.dc0, l.at, e, l.two);
   if (!a.dbias) return;
-  // sums of the waves, in order (lds.wave is 2 x kScanWaves rows of 64)
+  // sums of the waves, in order (lds.wave is 2 x W rows of 64)
   lds_barrier();
   lds.wave[0][wave][lane] = f32x4{si[0], si[1], sf[0], sf[1]};
   lds.wave[1][wave][lane] = f32x4{sg[0], sg[1], so[0], so[1]};
@@ -535,7 +531,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) linear_back_kernel(LinearArgs
   if (wave < 2 && l.live) {
     f32x4 t = lds.wave[wave][0][lane];
 #pragma unroll
-    for (int v = 1; v < kScanWaves; ++v) t += lds.wave[wave][v][lane];
+    for (int v = 1; v < W; ++v) t += lds.wave[wave][v][lane];
     float* row = a.dpart + ((size_t)(LOOK ? order : 0) * a.B + l.b) * (4 * (size_t)a.H) + (size_t)2 * wave * a.H + l.r;
     row[0] = t[0], row[a.H] = t[2];
     if (l.two) row[1] = t[1], row[a.H + 1] = t[3];
@@ -573,7 +569,7 @@ __global__ void __launch_bounds__(256) linear_clear_kernel(u32x4* words, size_t 
 
 struct Plan {
   LinearScan s;
-  bool walk, look, fits;
+  bool few, walk, look, fits;
   size_t lanes;          // pairs of units
   size_t maps, states, tickets, dpart;   // bytes
   int rows;              // of dpart
@@ -585,8 +581,10 @@ Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   p.lanes = (size_t)B * pairs;
   p.s.lanes = (int)p.lanes;
   p.s.cols = (int)((p.lanes + 63) / 64);
-  p.s.chunks = std::max(1, (T + kChunk - 1) / kChunk);
-  p.walk = !backward && T <= 16;
+  p.few = T <= 16;
+  const int chunk = backward && p.few ? 16 : kChunk;
+  p.s.chunks = std::max(1, (T + chunk - 1) / chunk);
+  p.walk = !backward && p.few;
   // Forward, chunks side by side where there are at least four and the columns
   // alone leave compute units with fewer than two workgroups (bf16, H = 512, T = 512,
   // side by side / one after another: 64 sequences 46 / 46 us, 128 89 / 78, 256 162 /
@@ -635,9 +633,11 @@ void launch_run(const LinearArgs& a, const Plan& p, hipStream_t stream) {
 template <class T, Rows R>
 void launch_back(const LinearArgs& a, const Plan& p, hipStream_t stream) {
   if (p.look)
-    linear_back_kernel<T, R, true><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+    linear_back_kernel<T, R, true, kScanWaves><<<(unsigned)p.s.cols * p.s.chunks, kScanThreads, 0, stream>>>(a, p.s);
+  else if (p.few)
+    linear_back_kernel<T, R, false, 2><<<p.s.cols, 128, 0, stream>>>(a, p.s);
   else
-    linear_back_kernel<T, R, false><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
+    linear_back_kernel<T, R, false, kScanWaves><<<p.s.cols, kScanThreads, 0, stream>>>(a, p.s);
 }
 
 // f of a's kind of rows
