@@ -32,7 +32,6 @@ namespace alstm {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
@@ -205,14 +204,7 @@ struct Parts<float> {
 __device__ __forceinline__ float sum8(const f32x8& v) {
   return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
-__device__ __forceinline__ float sum8(const bf16x8& v) {
-  const u32x4 w = __builtin_bit_cast(u32x4, v);
-  const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), one, s, false);
-  return s;
-}
+__device__ __forceinline__ float sum8(const bf16x8& v) { return sum8(__builtin_convertvector(v, f32x8)); }
 
 // scales and moved zero levels of four rows
 struct Scale {
