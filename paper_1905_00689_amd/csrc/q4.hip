@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
 }
 
 // Many rows of x: a matrix product.  A workgroup takes 256 rows of the matrix and 64
-// of x; its four waves 64 rows each, whose levels go from the store to operands
+// or 32 of x; its four waves 64 rows each, whose levels go from the store to operands
 // without LDS (nobody else needs them), while x, which all four need, is staged
 // there a block of columns at a time, the next block's loads under way meanwhile.  The
 // group sums of x are formed by the threads that stage it.
@@ -433,12 +433,11 @@ struct TileLds {
 };
 
 template <class T, int G, int NT>
-__global__ void __launch_bounds__(kTileThreads, NT == 4 ? 2 : 3) q4_tile_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y,
+__global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 3) q4_tile_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y,
                                                                int row_blocks, int x_blocks) {
   constexpr int RT = 4, kTileX = 16 * NT, kSteps = kBlockCols / 32, kGroupSteps = G / 32, kGroups = kBlockCols / G,
                 kParts = Parts<T>::kParts, kChunks = kTileX * kBlockCols / 8 / kTileThreads;
-  constexpr int kBuffers = kParts == 1 ? 2 : 1;   // (two of fp32's would leave room for one workgroup)
-  __shared__ TileLds<T, G, kTileX> lds[kBuffers];
+  __shared__ TileLds<T, G, kTileX> lds[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   // consecutive workgroups go to the 8 XCDs in turn: an XCD takes whole blocks of x
@@ -480,8 +479,7 @@ __global__ void __launch_bounds__(kTileThreads, NT == 4 ? 2 : 3) q4_tile_kernel(
     for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   load(0);
   for (int kb = 0; kb < m.blocks; ++kb) {
-    TileLds<T, G, kTileX>& l = lds[kb % kBuffers];
-    if (kBuffers == 1) lds_barrier();
+    TileLds<T, G, kTileX>& l = lds[kb % 2];
     u32x4 now[RT];
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
@@ -567,17 +565,32 @@ void launch_dot(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, h
 
 template <class T, int G>
 void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, int num_cu, hipStream_t stream) {
-  // the tile kernel from a workgroup per compute unit on; below, the widest shape of
-  // the row kernel that still has one
+  // What both sides took, in us, D = 2048 unless given:
+  // - many rows of x: the tile kernel once half the compute units get a workgroup of it
+  //   (a workgroup takes as long as 16 blocks of columns do, 24 in bf16, 40 in fp32; the
+  //   row kernel's time grows with the rows), 64 rows of x at a time where that makes two
+  //   a unit (bf16, 4096 x 2048: 64 at a time 49, 32 54; 2048 x 2048: 36, 32), in fp32
+  //   always 32 (8192 x 2048: 214, 64 at a time 254 with spilled registers).  Row kernel
+  //   / tile kernel: bf16, R = 2048, N = 512 22 / 24, N = 1024 42 / 24; R = 8192, N = 256
+  //   42 / 26; fp32, R = 2048, N = 256 24 / 40, N = 512 46 / 40, N = 1024 89 / 41.
+  // - one row, in fp32 two: the dot kernel (fp32, G = 32, R = 32768, D = 8192: 40, row
+  //   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
+  //   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
+  //   D = 8256: 8.4, eight waves 14).
+  // - else the row kernel, in the widest shape that still has a workgroup a unit (fp32,
+  //   R = 256, D = 8256, N = 100: 16 x 16 23, 32 x 64 87).
   const size_t tiles = m.tiles, cu = num_cu;
   auto cover = [](size_t n, size_t by) { return (n + by - 1) / by; };
-  if (N > 64 && cover(m.R, kTileRows) * cover(N, 64) >= 2 * cu) launch_tile<T, G, 4>(m, x, N, bias, y, stream);
-  else if (N > 64 && cover(m.R, kTileRows) * cover(N, 32) >= (sizeof(T) == 2 ? cu / 2 + 1 : cu)) launch_tile<T, G, 2>(m, x, N, bias, y, stream);
+  constexpr bool kHalf = sizeof(T) == 2;
+  const size_t wide = cover(m.R, kTileRows) * cover(N, 64), narrow = cover(m.R, kTileRows) * cover(N, 32);
+  if constexpr (kHalf)
+    if (N > 64 && wide >= 2 * cu) return launch_tile<T, G, 4>(m, x, N, bias, y, stream);
+  if (N > 64 && 2 * narrow >= cu + kHalf) launch_tile<T, G, 2>(m, x, N, bias, y, stream);
   else if (N == 1 && tiles >= 4 * cu) launch_dot<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
   else if (N == 1 && tiles >= 2 * cu) launch_dot<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
   else if (N == 1) launch_dot<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
-  else if (N == 2 && sizeof(T) == 4 && tiles >= 2 * cu) launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
-  else if (N == 2 && sizeof(T) == 4) launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
+  else if (N == 2 && !kHalf && tiles >= 2 * cu) launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+  else if (N == 2 && !kHalf) launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
   else if (N <= 16 && tiles >= 4 * cu) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
   else if (N > 32 && cover(tiles, 2) * cover(N, 64) >= cu) launch_rows<T, G, 2, 4, 8>(m, x, N, bias, y, stream);
   else if (N > 16 && cover(tiles, 2) * cover(N, 32) >= cu) launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
