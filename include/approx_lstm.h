@@ -570,7 +570,7 @@ approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H,
  * else in the high half; scale device fp32 [rows][ceil(cols / G)]; zero device
  * uint8 [rows][ceil(cols / G)], each at most 15 (else INVALID_ARG), or NULL: 8
  * everywhere.
- *   rows, cols   at least 1
+ *   rows, cols   at least 1; more than 2^25 rows or 2^30 columns are UNSUPPORTED
  *   group        G: 32, 64 or 128 (the last group of a row may be cut short)
  * Both synchronise hip_stream; the arrays may be freed afterwards.
  * approx_lstm_q4_get -- the stored matrix as host arrays in the formats of

@@ -1802,6 +1802,8 @@ approx_lstm_status approx_lstm_q4_load(const uint8_t* q, const float* scale, con
   g_last_error.clear();
   if (!q || !scale || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
   if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (rows > 1 << 25 || cols > 1 << 30)
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "more than 2^25 rows or 2^30 columns");
   if (group != 32 && group != 64 && group != 128)
     return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
   if (!aligned(scale, 4)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "scale not aligned to 4 bytes");
@@ -1840,6 +1842,8 @@ approx_lstm_status approx_lstm_q4_prepare(const float* w, int32_t rows, int32_t 
   g_last_error.clear();
   if (!w || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
   if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (rows > 1 << 25 || cols > 1 << 30)
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "more than 2^25 rows or 2^30 columns");
   if (group != 32 && group != 64 && group != 128)
     return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
   const size_t R = rows, D = cols, groups = (D + group - 1) / group, row_bytes = (D + 1) / 2;

@@ -125,6 +125,9 @@ def test_load_refusals(over):
     a.update(over)
     out = ctypes.c_void_p()
     assert B.lib.approx_lstm_q4_load(*a.values(), ctypes.byref(out)) == 1 and not out.value
+    for big in (dict(rows=(1 << 25) + 1), dict(cols=(1 << 30) + 1)):
+        assert B.lib.approx_lstm_q4_load(*dict(a, **dict(dict(q=P, scale=P, rows=4, cols=64, group=32), **big)).values(),
+                                         ctypes.byref(out)) == 6
 
 
 def test_prepare_refusals():

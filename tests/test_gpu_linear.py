@@ -171,6 +171,52 @@ def test_steps_and_pieces_join(T, Bn, H):
     near("h", two[:20], h[:20], he[:20], HALF[F32])
 
 
+@pytest.mark.parametrize("T,Bn,H", [(1, 3, 64), (30, 3, 33), (100, 2, 64), (3000, 2, 34)])
+def test_states_updated_in_place(T, Bn, H):
+    """c_out may be c0, and dc0 may be dc_out: the same bits as apart."""
+    say("in place", T, Bn, H)
+    k = Case(T, Bn, H)
+    o = k.out()
+    k.run(o)
+    k.back(o)
+    again = k.out()
+    c, dc = k.c0.clone(), k.dc.clone()
+    B.approx_lstm_linear_run(k.p, again["h"], bias=k.bias, c0=c, c_out=c, c_save=again["save"])
+    B.approx_lstm_linear_backward(k.p, k.dh, again["save"], again["dp"], bias=k.bias, dc_out=dc, dc0=dc,
+                                  dbias=again["db"])
+    assert torch.equal(c, o["c"]) and torch.equal(dc, o["dc0"])
+    assert all(torch.equal(again[n], o[n]) for n in ("h", "save", "dp", "db"))
+
+
+def test_offsets_past_2_31():
+    """p of 2.4e9 elements (4.8 GB): its last timesteps are those of a run that
+    begins at the state saved before them, and so are their gradients."""
+    T, H, tail = 300000, 2000, 600
+    g = torch.Generator(device="cuda").manual_seed(11)
+    p = torch.empty(T, 1, 4 * H, dtype=BF16, device="cuda")
+    for a in range(0, T, 10000):
+        p[a:a + 10000] = torch.randn(10000, 1, 4 * H, generator=g, device="cuda")
+    h, c = torch.empty(T, 1, H, dtype=BF16, device="cuda"), torch.empty(1, H, device="cuda")
+    save = torch.empty(T // 8, 1, H, device="cuda")
+    B.approx_lstm_linear_run(p, h, c_out=c, c_save=save)
+    at = T - tail
+    part, k = p[at:].contiguous(), Case(tail, 1, H, BF16, bias=False, state=False)
+    k.p, k.c0 = part, save[at // 8].contiguous()
+    o = k.out()
+    k.run(o)
+    want, cw, he, ce = gated.linear_lstm(k.host(part), None, None, k.host(k.c0))
+    near("h", h[at:], want, he, HALF[BF16])
+    near("c", c, cw[-1], ce[-1], HALF[F32])
+    near("save", save[at // 8:], cw[:-1][::8], ce[:-1][::8], HALF[F32])
+    del h
+    dh = torch.zeros(T, 1, H, dtype=BF16, device="cuda")
+    dh[at:] = k.dh
+    dp = torch.empty_like(p)
+    B.approx_lstm_linear_backward(p, dh, save, dp)
+    ref, err = gated.linear_lstm_grad(k.host(part), k.host(k.dh), None, None, None, k.host(k.c0))
+    near("dp", dp[at:], ref["dp"], err["dp"], HALF[BF16])
+
+
 def test_no_timesteps():
     c0, c = torch.randn(3, 8, device="cuda"), torch.empty(3, 8, device="cuda")
     p = torch.empty(0, 3, 32, device="cuda")

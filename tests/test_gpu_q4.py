@@ -44,7 +44,9 @@ def check(y, q, s, z, G, x, bias):
 SHAPES = [(1, 1, 1, 32), (1, 128, 64, 128), (1, 100, 77, 32), (2, 16, 128, 64), (3, 33, 129, 128), (5, 256, 2048, 128),
           (16, 48, 260, 32), (17, 64, 96, 64), (31, 129, 500, 128), (48, 300, 257, 64), (64, 20, 1000, 32),
           (65, 512, 64, 32), (100, 256, 1030, 32), (129, 130, 127, 64), (300, 272, 520, 128), (700, 96, 40, 32),
-          (1100, 4000, 200, 32), (2050, 2100, 300, 128), (4200, 1000, 129, 64), (70, 33000, 64, 32)]
+          (1100, 4000, 200, 32), (2050, 2100, 300, 128), (4200, 1000, 129, 64), (70, 33000, 64, 32),
+          (1, 8200, 200, 64), (2, 8200, 200, 64), (1, 16400, 130, 32), (5, 16400, 130, 32), (40, 8200, 300, 128),
+          (20, 8200, 300, 128)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
@@ -158,6 +160,20 @@ def test_refusals_on_the_device():
         B.approx_lstm_q4_run(m, x, y, bias=torch.zeros(7, device="cuda"))
     assert torch.isnan(y).all()
     B.approx_lstm_q4_run(m, x[:0], y[:0])
+
+
+def test_more_rows_than_a_launch_takes():
+    """1.1 million rows of x, and an output of more than 2^31 elements: the last
+    rows are those of a small call."""
+    for N, D, R, dtype in ((1100000, 40, 20, F32), (40000, 33, 60000, BF16)):
+        q, s, z = levels(R, D, 32)
+        m = load(q, s, z, 32)
+        x = torch.randn(N, D, device="cuda").to(dtype)
+        y = torch.empty(N, R, dtype=dtype, device="cuda")
+        B.approx_lstm_q4_run(m, x, y)
+        for rows in (slice(0, 3), slice(N // 2, N // 2 + 3), slice(N - 3, N)):
+            check(y[rows].contiguous(), q, s, z, 32, x[rows], None)
+        del x, y
 
 
 def test_layer_of_product_and_recurrence():
