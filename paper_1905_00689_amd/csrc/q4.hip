@@ -577,8 +577,11 @@ void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y,
   //   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
   //   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
   //   D = 8256: 8.4, eight waves 14).
-  // - else the row kernel, in the widest shape that still has a workgroup a unit (fp32,
-  //   R = 256, D = 8256, N = 100: 16 x 16 23, 32 x 64 87).
+  // - else the row kernel, in the widest shape that still has a workgroup a unit: fp32,
+  //   R = 8192, N = 12: 32 x 16 7.2, 64 x 16 10.4; N = 48 64 x 32 15, 32 x 64 19; R = 256,
+  //   D = 8256, N = 100: 16 x 16 23, 32 x 64 87.  Below that 16 x 16 on sixteen waves, but
+  //   32 x 32 once they do not all run at once (bf16, G = 32, R = 1000, D = 2000, N = 200:
+  //   13 and 7.8; R = 2048, D = 4096, N = 64, two a unit: 10.4 and 11.9).
   const size_t tiles = m.tiles, cu = num_cu;
   auto cover = [](size_t n, size_t by) { return (n + by - 1) / by; };
   constexpr bool kHalf = sizeof(T) == 2;
@@ -592,8 +595,10 @@ void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y,
   else if (N == 2 && !kHalf && tiles >= 2 * cu) launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
   else if (N == 2 && !kHalf) launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
   else if (N <= 16 && tiles >= 4 * cu) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
-  else if (N > 32 && cover(tiles, 2) * cover(N, 64) >= cu) launch_rows<T, G, 2, 4, 8>(m, x, N, bias, y, stream);
-  else if (N > 16 && cover(tiles, 2) * cover(N, 32) >= cu) launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+  else if (N <= 16 && tiles >= 2 * cu) launch_rows<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
+  else if (N > 16 && cover(tiles, 4) * cover(N, 32) >= cu) launch_rows<T, G, 4, 2, 8>(m, x, N, bias, y, stream);
+  else if (N > 16 && (cover(tiles, 2) * cover(N, 32) >= cu || tiles * cover(N, 16) > 2 * cu))
+    launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
   else launch_rows<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
 }
 
