@@ -241,7 +241,12 @@ __device__ __forceinline__ void store_y(T* y, const float* bias, int R, size_t n
 
 // Few rows of x: what bounds it is reading the matrix, so every workgroup reads RT
 // row tiles of it once, its KW waves every KW-th block of columns, for up to 16 NT
-// rows of x straight from L2; the waves' sums meet in LDS, in order.
+// rows of x straight from L2; the waves' sums meet in LDS, in order.  A few blocks a wave
+// leave it to latency: 48 rows of x, 8192 x 2048, bf16 10.7 us (10 MB and 0.4 MB of
+// scales); 16 rows, 32768 x 8192 39 us (145 MB, 3.7 TB/s).  fp32 is bound by splitting x
+// (44 operations a step of 32 columns, 22 for the levels): 100 rows of 8256 columns, 256
+// rows of the matrix, G = 32: 22 us on 112 compute units.  Loading x a block ahead too
+// changes nothing.
 template <class T, int G, int RT, int NT, int KW>
 __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y) {
   constexpr int kSteps = kBlockCols / 32, kGroupSteps = G / 32, kParts = Parts<T>::kParts;
@@ -332,7 +337,8 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
 // One or two rows of x in fp32: with 14 of 16 columns of an operand idle, splitting x
 // and centring the levels costs more than multiplying on the vector units.  A lane
 // has the row of the matrix and the columns that its words hold; its products begin
-// at -z sum x, so that they end up no larger than they have to be.
+// at -z sum x, so that they end up no larger than they have to be.  32768 x 8192, fp32:
+// 32.5 us for 145 MB (4.5 TB/s; cached loads of the levels 35 us, the row kernel 59).
 template <class T, int G, int RT, int NX, int KW>
 __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y) {
   constexpr int kSteps = kBlockCols / 32, kGroupSteps = G / 32, kGroups = kBlockCols / G;
@@ -420,7 +426,12 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
 // or 32 of x; its four waves 64 rows each, whose levels go from the store to operands
 // without LDS (nobody else needs them), while x, which all four need, is staged
 // there a block of columns at a time, the next block's loads under way meanwhile.  The
-// group sums of x are formed by the threads that stage it.
+// group sums of x are formed by the threads that stage it, and the scales stand beside
+// them.  4096 rows of x, 2048 x 2048, bf16, G = 128: 46 us (750 TFLOP/s, a large library
+// product in bf16 1210); R = 8192 169 us (815).  A wave's block is 64 matrix
+// instructions (1024 cycles) and 380 others (1500): bound by those and, at two
+// waves a unit, by the wait for the next block of x.  Tried: loads two blocks ahead in
+// registers (spills: 57 us); scales read at the end of a group instead of staged (67).
 constexpr int kTileRows = 256, kTileThreads = 256;
 constexpr int kTileLd = kBlockCols + 8;   // LDS row (bf16): 16-byte reads of 16 rows in distinct banks
 

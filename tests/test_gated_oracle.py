@@ -95,7 +95,8 @@ def run_args(**over):
 @pytest.mark.parametrize("over,status", [
     (dict(p=None), 1), (dict(h=None), 1), (dict(T=-1), 1), (dict(B=0), 1), (dict(H=0), 1), (dict(dtype=2), 1),
     (dict(dtype=-1), 1), (dict(p=ODD), 1), (dict(h=ODD, dtype=1), 1), (dict(bias=ODD), 1), (dict(lengths=ODD), 1),
-    (dict(c0=ODD), 1), (dict(c_out=ODD), 1), (dict(c_save=ODD), 1), (dict(B=1 << 20, H=1 << 10), 6)])
+    (dict(c0=ODD), 1), (dict(c_out=ODD), 1), (dict(c_save=ODD), 1), (dict(B=1 << 20, H=1 << 10), 6),
+    (dict(T=(1 << 31) - 1), 6)])
 def test_run_refusals(over, status):
     assert B.lib.approx_lstm_linear_run(*run_args(**over)) == status
     assert B.approx_lstm_last_error()

@@ -91,7 +91,8 @@ def check(k, o):
 
 
 SHAPES = [(1, 1, 1), (1, 5, 64), (2, 1, 3), (7, 3, 65), (8, 1, 128), (9, 2, 130), (17, 4, 31), (63, 1, 64),
-          (64, 2, 129), (65, 1, 2), (100, 1, 64), (129, 3, 50), (500, 2, 257), (2100, 1, 70), (4500, 1, 2)]
+          (64, 2, 129), (65, 1, 2), (100, 1, 64), (129, 3, 50), (500, 2, 257), (2100, 1, 70), (4500, 1, 2),
+          (700, 2, 1), (16, 3, 40)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
@@ -106,7 +107,7 @@ def test_run_and_gradients(T, Bn, H, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("T,H", [(40, 33), (200, 64), (1100, 20)])
+@pytest.mark.parametrize("T,H", [(9, 33), (16, 64), (40, 33), (200, 64), (1100, 20)])
 def test_lengths(T, H, dtype):
     """Sequences of none, some and all timesteps (and lengths out of range); NaN
     in the padding reaches nothing, and its outputs are zeros."""
@@ -325,6 +326,37 @@ def test_two_streams_at_once():
         assert all(torch.equal(o[n], w[n]) for n in o)
 
 
+@pytest.mark.parametrize("T", [5, 700])
+def test_streams_given_as_handles_and_workspace_from_torch(T):
+    """A side stream current and the default one given by its handle, the other
+    way round, and a graph captured without a workspace of the caller's."""
+    k = Case(T, 2, 64, seed=9)
+    want = k.out()
+    k.run(want)
+    k.back(want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for current, given in ((side, 0), (torch.cuda.default_stream(), side.cuda_stream)):
+        o = k.out()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(current):
+            k.run(o, stream=given)
+            k.back(o, stream=given)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[n], want[n]) for n in o)
+    o = k.out()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        k.run(o)
+        k.back(o)
+    for _ in range(3):
+        for t in o.values():
+            t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[n], want[n]) for n in o)
+
+
 def test_refusals_on_the_device():
     k = Case(300, 2, 64)
     o = k.out()
@@ -343,3 +375,7 @@ def test_refusals_on_the_device():
     with pytest.raises(TypeError):
         B.approx_lstm_linear_run(k.p.half(), o["h"])
     assert all(torch.isnan(t).all() for t in o.values())
+    # more pieces than a backward pass takes (refused before anything is looked at)
+    at = k.p.data_ptr()
+    assert B.lib.approx_lstm_linear_backward(at, None, (1 << 28) + 1, 1, 2, 0, None, at, at, None, at, None, None,
+                                             None, 0, None) == 6
