@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
 // Many rows of x: a matrix product.  A workgroup takes 256 rows of the matrix and 64
 // or 32 of x; its four waves 64 rows each, whose levels go from the store to operands
 // without LDS (nobody else needs them), while x, which all four need, is staged
-// there a block of columns at a time, the next block's loads under way meanwhile.  The
+// there a block of columns at a time, the next block's loads under way meanwhile; with
+// KS = 2 there are eight, the second four on every other block of columns.  The
 // group sums of x are formed by the threads that stage it, and the scales stand beside
 // them.  4096 rows of x, 2048 x 2048, bf16, G = 128: 46 us (750 TFLOP/s, a large library
 // product in bf16 1210); R = 8192 169 us (815).  A wave's block is 64 matrix
@@ -443,13 +444,15 @@ struct TileLds {
   float sum[kBlockCols / G][X];                     // group sums of x
 };
 
-template <class T, int G, int NT>
-__global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 3) q4_tile_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y,
+template <class T, int G, int NT, int KS>
+__global__ void __launch_bounds__(kTileThreads * KS, NT == 4 || KS == 2 || sizeof(T) == 4 ? 2 : 3)
+    q4_tile_kernel(Q4Matrix m, const T* x, int N, const float* bias, T* y,
                                                                int row_blocks, int x_blocks) {
   constexpr int RT = 4, kTileX = 16 * NT, kSteps = kBlockCols / 32, kGroupSteps = G / 32, kGroups = kBlockCols / G,
                 kParts = Parts<T>::kParts, kChunks = kTileX * kBlockCols / 8 / kTileThreads;
-  __shared__ TileLds<T, G, kTileX> lds[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ TileLds<T, G, kTileX> lds[KS][2];
+  const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / kTileThreads), tid = threadIdx.x % kTileThreads;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lg = lane >> 4;
   // consecutive workgroups go to the 8 XCDs in turn: an XCD takes whole blocks of x
   const int b = blockIdx.x, xb = (b % 8) + 8 * (b / (8 * row_blocks)), rb = (b / 8) % row_blocks;
@@ -488,9 +491,10 @@ __global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  load(0);
-  for (int kb = 0; kb < m.blocks; ++kb) {
-    TileLds<T, G, kTileX>& l = lds[kb % 2];
+  load(min(part, m.blocks - 1));
+  for (int it = 0; it * KS < m.blocks; ++it) {
+    const int kb = it * KS + part;
+    TileLds<T, G, kTileX>& l = lds[part][it % 2];
     u32x4 now[RT];
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
@@ -509,7 +513,8 @@ __global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 
 #pragma unroll
     for (int r = 0; r < RT; ++r) now[r] = w[r];
     lds_barrier();
-    if (kb + 1 < m.blocks) load(kb + 1);
+    if (kb >= m.blocks) break;   // (in the last round alone)
+    if (kb + KS < m.blocks) load(kb + KS);
     f32x4 p[RT][NT];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -548,6 +553,18 @@ __global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 
       }
     }
   }
+  if constexpr (KS == 2) {   // the second half's sums onto the first's, through the buffers
+    static_assert(sizeof(lds) >= sizeof(f32x4) * 64 * 4 * RT * NT, "room for the sums");
+    f32x4(*sums)[RT * NT][64] = reinterpret_cast<f32x4(*)[RT * NT][64]>(&lds);
+    lds_barrier();
+    if (part == 1)
+#pragma unroll
+      for (int j = 0; j < RT * NT; ++j) sums[wave][j][lane] = acc[j / NT][j % NT];
+    lds_barrier();
+    if (part == 1) return;
+#pragma unroll
+    for (int j = 0; j < RT * NT; ++j) acc[j / NT][j % NT] += sums[wave][j][lane];
+  }
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -557,10 +574,10 @@ __global__ void __launch_bounds__(kTileThreads, NT == 4 || sizeof(T) == 4 ? 2 : 
     }
 }
 
-template <class T, int G, int NT>
+template <class T, int G, int NT, int KS>
 void launch_tile(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, hipStream_t stream) {
   const int rb = (m.R + kTileRows - 1) / kTileRows, xb = (N + 16 * NT - 1) / (16 * NT);
-  q4_tile_kernel<T, G, NT><<<(unsigned)((xb + 7) / 8 * 8 * rb), kTileThreads, 0, stream>>>(m, x, N, bias, y, rb, xb);
+  q4_tile_kernel<T, G, NT, KS><<<(unsigned)((xb + 7) / 8 * 8 * rb), kTileThreads * KS, 0, stream>>>(m, x, N, bias, y, rb, xb);
 }
 
 template <class T, int G, int RT, int NT, int KW>
@@ -577,13 +594,14 @@ void launch_dot(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, h
 template <class T, int G>
 void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, int num_cu, hipStream_t stream) {
   // What both sides took, in us, D = 2048 unless given:
-  // - many rows of x: the tile kernel once half the compute units get a workgroup of it
-  //   (a workgroup takes as long as 16 blocks of columns do, 24 in bf16, 40 in fp32; the
-  //   row kernel's time grows with the rows), 64 rows of x at a time where that makes two
-  //   a unit (bf16, 4096 x 2048: 64 at a time 49, 32 54; 2048 x 2048: 36, 32), in fp32
-  //   always 32 (8192 x 2048: 214, 64 at a time 254 with spilled registers).  Row kernel
-  //   / tile kernel: bf16, R = 2048, N = 512 22 / 24, N = 1024 42 / 24; R = 8192, N = 256
-  //   42 / 26; fp32, R = 2048, N = 256 24 / 40, N = 512 46 / 40, N = 1024 89 / 41.
+  // - many rows of x: the tile kernel once half the compute units get a workgroup of it;
+  //   64 rows of x at a time where that makes two a unit (bf16, 4096 x 2048: 49, 32 at a
+  //   time 54; 2048 x 2048: 36 and 31), in fp32 always 32 (8192 x 2048: 211, 64 at a time
+  //   254 with spilled registers); the columns in two halves where there is at most a
+  //   workgroup a unit (R = 2048, N = 1024, bf16 19, whole 23, fp32 34 and 40; R = 3716, D =
+  //   2951, N = 730, 345 workgroups: 52 and 45).  Row kernel / tile kernel: R = 2048, N =
+  //   256, bf16 9 / 18, fp32 15 / 31; N = 512 16.5 / 18.7, 46 / 31; N = 1024 42 / 19, 89 / 34;
+  //   R = 256, D = 4096, N = 4096 50 / 36, 76 / 63.
   // - one row, in fp32 two: the dot kernel (fp32, G = 32, R = 32768, D = 8192: 40, row
   //   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
   //   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
@@ -598,8 +616,9 @@ void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y,
   constexpr bool kHalf = sizeof(T) == 2;
   const size_t wide = cover(m.R, kTileRows) * cover(N, 64), narrow = cover(m.R, kTileRows) * cover(N, 32);
   if constexpr (kHalf)
-    if (N > 64 && wide >= 2 * cu) return launch_tile<T, G, 4>(m, x, N, bias, y, stream);
-  if (N > 64 && 2 * narrow >= cu + kHalf) launch_tile<T, G, 2>(m, x, N, bias, y, stream);
+    if (N > 64 && wide >= 2 * cu) return launch_tile<T, G, 4, 1>(m, x, N, bias, y, stream);
+  if (N > 64 && narrow > cu) launch_tile<T, G, 2, 1>(m, x, N, bias, y, stream);
+  else if (N > 64 && 2 * narrow >= cu) launch_tile<T, G, 2, 2>(m, x, N, bias, y, stream);
   else if (N == 1 && tiles >= 4 * cu) launch_dot<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
   else if (N == 1 && tiles >= 2 * cu) launch_dot<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
   else if (N == 1) launch_dot<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
