@@ -131,7 +131,11 @@ __device__ __forceinline__ bf16x8 levels_centred(unsigned w) {
 }
 
 // Eight values of a row of x from column k, zeros past its end; `whole`: none is.
-// (Loads of these types need be aligned to their elements only.)
+// Loads of these types need be aligned to their elements only, but a load that is not
+// aligned to 4 bytes takes several times as long: where rows of bf16 begin at odd
+// elements (`odd`), a lane loads the words that its values stand in, which all hold one
+// of them, and shifts (row kernel, 16 rows, 2048 x 7507: 13 us, without 22; the tile
+// kernel, whose threads load little at a time, is slower with it: 2000 rows, 44 and 37).
 template <class T>
 struct XVec;
 template <>
@@ -145,11 +149,32 @@ struct XVec<float> {
   typedef f32x8 Any __attribute__((aligned(4)));
 };
 template <class T>
-__device__ __forceinline__ typename XVec<T>::Raw load_x(const T* row, int k, int D, bool whole) {
-  if (whole) return *reinterpret_cast<const typename XVec<T>::Any*>(row + k);
+__device__ __forceinline__ typename XVec<T>::Raw load_eight(const T* p, bool odd) {
+  if constexpr (sizeof(T) == 2) {
+    if (odd) {
+      typedef u32x4 Words __attribute__((aligned(4)));
+      const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(p) & 2u), shift = 8 * off;
+      const unsigned* w = reinterpret_cast<const unsigned*>(reinterpret_cast<const char*>(p) - off);
+      const u32x4 v = *reinterpret_cast<const Words*>(w);
+      const unsigned last = w[off ? 4 : 3];
+      return __builtin_bit_cast(
+          bf16x8, u32x4{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift),
+                        __builtin_amdgcn_alignbit(v[3], v[2], shift), __builtin_amdgcn_alignbit(last, v[3], shift)});
+    }
+  }
+  return *reinterpret_cast<const typename XVec<T>::Any*>(p);
+}
+template <class T>
+__device__ __forceinline__ bool odd_rows(const T* x, int D) {
+  return sizeof(T) == 2 && ((D & 1) || (reinterpret_cast<uintptr_t>(x) & 2u));
+}
+
+template <class T>
+__device__ __forceinline__ typename XVec<T>::Raw load_x(const T* row, int k, int D, bool whole, bool odd) {
+  if (whole) return load_eight<T>(row + k, odd);
   typename XVec<T>::Raw v{};
   if (k + 8 <= D) {
-    v = *reinterpret_cast<const typename XVec<T>::Any*>(row + k);
+    v = load_eight<T>(row + k, odd);
   } else if (k < D) {   // (eight loads at once, not one after another)
     T t[8];
 #pragma unroll
@@ -254,6 +279,7 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int tile0 = blockIdx.x * RT, n0 = blockIdx.y * (16 * NT);
+  const bool odd = odd_rows(x, m.D);
   const T* row[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) row[t] = x + (size_t)min(n0 + 16 * t + li, N - 1) * m.D;
@@ -277,7 +303,7 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) xr[s][t] = load_x<T>(row[t], kb * kBlockCols + 8 * lg + 32 * s, m.D, whole);
+      for (int t = 0; t < NT; ++t) xr[s][t] = load_x<T>(row[t], kb * kBlockCols + 8 * lg + 32 * s, m.D, whole, odd);
     u32x4 now[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) now[r] = w[r];
@@ -345,6 +371,7 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
   __shared__ float part[KW][RT * NX][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4, tile0 = blockIdx.x * RT;
+  const bool odd = odd_rows(x, m.D);
   float acc[RT][NX] = {};
   const unsigned* wp[RT];
   size_t at_scale[RT];
@@ -378,7 +405,7 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
     for (int k = 0; k < kSteps; ++k)
 #pragma unroll
       for (int n = 0; n < NX; ++n) {
-        xv[k][n] = __builtin_convertvector(load_x<T>(x + (size_t)min(n, N - 1) * m.D, k0 + 32 * k, m.D, whole), f32x8);
+        xv[k][n] = __builtin_convertvector(load_x<T>(x + (size_t)min(n, N - 1) * m.D, k0 + 32 * k, m.D, whole, odd), f32x8);
         sum[k][n] = sum8(xv[k][n]);
       }
 #pragma unroll
@@ -477,7 +504,7 @@ __global__ void __launch_bounds__(kTileThreads * KS, NT == 4 || KS == 2 || sizeo
   auto load = [&](int kb) {
     const bool whole = (kb + 1) * kBlockCols <= m.D;
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) xr[j] = load_x<T>(row[j], kb * kBlockCols + col[j], m.D, whole);
+    for (int j = 0; j < kChunks; ++j) xr[j] = load_x<T>(row[j], kb * kBlockCols + col[j], m.D, whole, false);
 #pragma unroll
     for (int r = 0; r < RT; ++r) w[r] = *reinterpret_cast<const u32x4*>(wp[r] + (size_t)kb * 256);
 #pragma unroll
