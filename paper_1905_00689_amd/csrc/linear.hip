@@ -227,7 +227,8 @@ constexpr f32x4 kIdentity{1.f, 0.f, 1.f, 0.f};
 // block of the group (kScanWaves blocks, 4096 timesteps), and one waits for the
 // state that the group before handed on: a hop of the serial chain passes a whole
 // group, and a chunk reads 7 maps on average.  (One level of 32 chunks, 16 maps on
-// average, took 121 us instead of 113 at T = 65536, H = 512, bf16.)
+// average, took 121 us instead of 113 at T = 65536, H = 512, bf16; then one lane that
+// looks for a wave instead of all 64 brought it to 96.)
 //
 // Which chunk a workgroup takes is the ticket of its column: in the order in which
 // workgroups start, so the chunks that anyone waits for have workgroups that run.
