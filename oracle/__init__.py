@@ -22,8 +22,11 @@ What it computes follows "Approximate LSTMs for Time-Constrained Inference"
                      level or per-timestep schedule.
 * ``opcount``     -- the per-gate operation counts of Sec. III and Sec. VI-B
                      and the Table I efficiency arithmetic.
+* ``gated``       -- the gated linear recurrence with its gradients and the 4-bit
+                     gate product, with bounds on fp32 errors (pinned by
+                     ``tests/test_gated_oracle.py``).
 
-Every function is pinned by ``tests/test_oracle_pins.py`` against library
+Every other function is pinned by ``tests/test_oracle_pins.py`` against library
 routines, closed forms, invariants, brute force and the paper's printed
 numbers (no function here is "parity unpinned").
 """
