@@ -528,7 +528,8 @@ void approx_lstm_exact_destroy(approx_lstm_exact* m);
  * dp must not overlap the other arrays.
  *
  * approx_lstm_linear_workspace -- bytes of workspace of a run (backward = 0), of
- * a backward pass without (1) or with dbias (2) on the current device.
+ * a backward pass without (1) or with dbias (2) on the current device; sizes that
+ * such a call refuses in both types are refused here alike.
  *
  * Long sequences are spread over workgroups that hand states on.  They take their
  * places in the order in which they start, so nobody waits for one that has not

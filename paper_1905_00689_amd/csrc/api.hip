@@ -1708,24 +1708,32 @@ approx_lstm_status current_cus(int* num_cu) {
 
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+// The sizes that a run (backward 0) or a backward pass takes, with elements of `el`
+// bytes: looked at before anything is computed from them.
+approx_lstm_status check_linear_sizes(int T, int B, int H, size_t el, int backward) {
+  if (B < 1 || H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need B >= 1 and H >= 1");
+  if ((uint64_t)B * H >= (1ull << 31) / (4 * el))   // (a product of two int32 and no more: 64 bits hold it)
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "B = %d, H = %d: a timestep of 2 GiB or more", B, H);
+  if (T > INT32_MAX - 1024) return fail(APPROX_LSTM_ERR_UNSUPPORTED, "T = %d exceeds 2^31 - 1025", T);
+  if (!alstm::linear_fits(T, B, H, backward))
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "a backward pass of more than 2^22 pieces of 64 timesteps of 128 units");
+  return APPROX_LSTM_OK;
+}
+
 // Checks what a run and a backward pass have in common, and fills a's num_cu.
 approx_lstm_status check_linear(alstm::LinearArgs& a, int dtype, int backward, const void* ws, uint64_t ws_bytes) {
-  if (a.B < 1 || a.H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need B >= 1 and H >= 1");
   if (dtype != 0 && dtype != 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "dtype = %d is neither 0 nor 1", dtype);
   const size_t el = dtype ? 2 : 4;
-  if ((uint64_t)a.B * a.H * 4 * el >= (1ull << 31))
-    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "B = %d, H = %d: a timestep of 2 GiB or more", a.B, a.H);
-  if (a.T > INT32_MAX - 1024) return fail(APPROX_LSTM_ERR_UNSUPPORTED, "T = %d exceeds 2^31 - 1025", a.T);
+  approx_lstm_status st = check_linear_sizes(a.T, a.B, a.H, el, backward);
+  if (st != APPROX_LSTM_OK) return st;
   for (const void* p : {a.p, (const void*)a.h, a.dh, (const void*)a.dp})
     if (!aligned(p, el)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "p, h or a gradient not aligned to its elements");
   for (const void* p : {(const void*)a.bias, (const void*)a.lengths, (const void*)a.c0, (const void*)a.c_out,
                         (const void*)a.c_save, (const void*)a.dc_out, (const void*)a.dc0, (const void*)a.dbias})
     if (!aligned(p, 4)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "a state, bias, gradient or lengths not aligned to 4 bytes");
   a.bf16 = dtype;
-  approx_lstm_status st = current_cus(&a.num_cu);
+  st = current_cus(&a.num_cu);
   if (st != APPROX_LSTM_OK) return st;
-  if (!alstm::linear_fits(a.T, a.B, a.H, a.num_cu, backward))
-    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "a backward pass of more than 2^22 pieces of 64 timesteps of 128 units");
   const size_t need = alstm::linear_workspace(a.T, a.B, a.H, a.num_cu, backward);
   if (need && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(APPROX_LSTM_ERR_INVALID_ARG, "workspace of %zu bytes, 16-byte aligned, needed (given: %llu)", need,
@@ -1786,12 +1794,12 @@ approx_lstm_status approx_lstm_linear_backward(const void* p, const float* bias,
 approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H, int32_t backward, uint64_t* bytes) {
   g_last_error.clear();
   if (!bytes) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null bytes");
-  if (T < 0 || B < 1 || H < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 0, B >= 1 and H >= 1");
-  if (T > INT32_MAX - 1024 || (uint64_t)B * H >= (1ull << 29))
-    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "sizes beyond those of a run");
+  if (T < 0) return fail(APPROX_LSTM_ERR_INVALID_ARG, "need T >= 0");
   if (backward < 0 || backward > 2) return fail(APPROX_LSTM_ERR_INVALID_ARG, "backward = %d not in 0..2", backward);
+  approx_lstm_status st = check_linear_sizes(T, B, H, 2, backward);   // (either type's: the smaller one's limit)
+  if (st != APPROX_LSTM_OK) return st;
   int num_cu = 0;
-  approx_lstm_status st = current_cus(&num_cu);
+  st = current_cus(&num_cu);
   if (st != APPROX_LSTM_OK) return st;
   *bytes = alstm::linear_workspace(T, B, H, num_cu, backward);
   return APPROX_LSTM_OK;

@@ -44,8 +44,8 @@ struct LinearScan {
 // Bytes of workspace of a run (backward 0), a backward pass (1) or one with the
 // bias gradient (2).
 size_t linear_workspace(int T, int B, int H, int num_cu, int backward);
-// Whether a call of these sizes can be launched.
-bool linear_fits(int T, int B, int H, int num_cu, int backward);
+// Whether a call of these sizes can be launched (4 B H below 2^30, T below 2^31 - 1024).
+bool linear_fits(int T, int B, int H, int backward);
 // Launches the recurrence, or its backward pass, with that workspace.
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_linear_backward(const LinearArgs& a, void* ws, hipStream_t stream);

@@ -584,21 +584,31 @@ __global__ void __launch_bounds__(256) linear_clear_kernel(u32x4* words, size_t 
 
 struct Plan {
   LinearScan s;
-  bool few, walk, look, fits;
+  bool few, walk, look;
   size_t lanes;          // pairs of units
   size_t maps, states, tickets, dpart;   // bytes
   int rows;              // of dpart
 };
 
+// columns of 64 pairs of units; chunks of time of one; both together (few: up to 16
+// timesteps, of which a backward pass makes one short chunk)
+constexpr int kFew = 16;
+size_t cols_of(int B, int H) { return ((size_t)B * ((H + 1) / 2) + 63) / 64; }
+int chunks_of(int T, int backward) {
+  const int chunk = backward && T <= kFew ? kFew : kChunk;
+  return std::max(1, (T + chunk - 1) / chunk);
+}
+size_t pieces_of(int T, int B, int H, int backward) { return cols_of(B, H) * chunks_of(T, backward); }
+
+// for sizes that linear_fits takes
 Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   Plan p{};
   const int pairs = (H + 1) / 2;
   p.lanes = (size_t)B * pairs;
   p.s.lanes = (int)p.lanes;
-  p.s.cols = (int)((p.lanes + 63) / 64);
-  p.few = T <= 16;
-  const int chunk = backward && p.few ? 16 : kChunk;
-  p.s.chunks = std::max(1, (T + chunk - 1) / chunk);
+  p.s.cols = (int)cols_of(B, H);
+  p.few = T <= kFew;
+  p.s.chunks = chunks_of(T, backward);
   p.walk = !backward && p.few;
   // Forward, chunks side by side where there are at least four and the columns
   // alone leave compute units with fewer than two workgroups (bf16, H = 512, T = 512,
@@ -607,10 +617,9 @@ Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   // Backward always: the loop needs more registers than there are (the same shapes
   // forward and back: 126 / 126, 249 / 259, 460 / 510 us).  A grid has fewer than 2^32
   // threads: beyond, forward takes the loop and backward is refused.
-  const size_t pieces = (size_t)p.s.cols * p.s.chunks;
+  const size_t pieces = pieces_of(T, B, H, backward);
   p.look = !p.walk && p.s.chunks > 1 &&
            (backward || (p.s.chunks >= 4 && p.s.cols < 2 * num_cu && pieces <= kMostChunks));
-  p.fits = !backward || pieces <= kMostChunks;
   if (p.look) {
     const size_t groups = (size_t)(p.s.chunks + kGroup - 1) / kGroup;
     p.maps = ((size_t)p.s.chunks + p.s.chunks / kScanWaves) * p.lanes * 16;
@@ -665,7 +674,7 @@ void rows_of(const LinearArgs& a, F f) {
 
 }  // namespace
 
-bool linear_fits(int T, int B, int H, int num_cu, int backward) { return plan_of(T, B, H, num_cu, backward).fits; }
+bool linear_fits(int T, int B, int H, int backward) { return !backward || pieces_of(T, B, H, backward) <= kMostChunks; }
 
 size_t linear_workspace(int T, int B, int H, int num_cu, int backward) {
   const Plan p = plan_of(T, B, H, num_cu, backward);

@@ -1,0 +1,36 @@
+"""Sizes that no call of the gated linear recurrence takes are refused before
+anything is computed from them, by the workspace query as by the calls (no GPU)."""
+
+import ctypes
+
+import pytest
+
+from paper_1905_00689_amd import binding as B
+
+P = ctypes.c_void_p(4096)      # an address that no refused call looks at
+
+
+def query(T, Bn, H, backward):
+    n = ctypes.c_uint64(77)
+    return B.lib.approx_lstm_linear_workspace(T, Bn, H, backward, ctypes.byref(n)), n.value
+
+
+# 4 B H elements of 2 bytes make 2 GiB from B H = 2^28; 2^30 x 2^30 x 16 bytes are 0 modulo 2^64
+@pytest.mark.parametrize("Bn,H", [(1 << 28, 1), (1, 1 << 28), (1 << 30, 1 << 30), (1 << 15, 1 << 15),
+                                  ((1 << 31) - 1, (1 << 31) - 1)])
+def test_timesteps_of_2_gib(Bn, H):
+    for dtype in (0, 1):
+        assert B.lib.approx_lstm_linear_run(P, None, 1, Bn, H, dtype, None, None, P, None, None, None, 0, None) == 6
+        assert B.lib.approx_lstm_linear_backward(P, None, 1, Bn, H, dtype, None, P, P, None, P, None, None, None, 0,
+                                                 None) == 6
+    for backward in (0, 1, 2):
+        assert query(1, Bn, H, backward) == (6, 77)
+
+
+@pytest.mark.parametrize("T,Bn,H", [(1 << 28, 1024, 2), ((1 << 28) + 1, 1, 2), (1 << 30, 1 << 20, 100),
+                                    ((1 << 31) - 1, 1, 1)])
+def test_backward_passes_of_too_many_pieces(T, Bn, H):
+    """T / 64 x B H / 128 above 2^22 (the first: B T / 64 = 2^32 rows of partial sums)."""
+    for backward in (1, 2):
+        assert query(T, Bn, H, backward) == (6, 77)
+    assert B.lib.approx_lstm_linear_backward(P, None, T, Bn, H, 1, None, P, P, None, P, None, P, None, 0, None) == 6
