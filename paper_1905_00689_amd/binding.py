@@ -421,6 +421,13 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _int32(n, name):
+    """n as the int32 that the C ABI takes (ctypes would cut it without a word)."""
+    if not -(1 << 31) <= n < 1 << 31:
+        raise ValueError(f"{name} = {n} does not fit 32 bits")
+    return n
+
+
 def _on(t, name, shape, dtype, index):
     """Device pointer of a contiguous tensor of that shape and type on GPU `index`."""
     if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
@@ -491,7 +498,10 @@ def _gates(p):
     shape = p.shape
     if len(shape) != 3 or shape[2] % 4 or not shape[2] or not shape[1]:
         raise ValueError(f"p has shape {tuple(shape)}, expected (T, B, 4 H)")
-    return shape[0], shape[1], shape[2] // 4, p.get_device(), _DTYPES[p.dtype]
+    T, B, H = shape[0], shape[1], shape[2] // 4
+    if max(T, B, H) >> 31:
+        raise ValueError(f"p has shape {tuple(shape)}: sizes of 2^31 and more are not taken")
+    return T, B, H, p.get_device(), _DTYPES[p.dtype]
 
 
 def approx_lstm_linear_run(p, h_out, bias=None, lengths=None, c0=None, c_out=None, c_save=None, workspace=None,
@@ -531,9 +541,10 @@ def approx_lstm_linear_backward(p, dh, c_save, dp, bias=None, lengths=None, dc_o
 def approx_lstm_linear_workspace(T, B, H, backward=0, device=None):
     """Bytes of workspace of a run (backward 0) or of a backward pass without (1)
     or with dbias (2), on `device` (None: the current one)."""
+    sizes = [_int32(int(n), name) for n, name in ((T, "T"), (B, "B"), (H, "H"), (backward, "backward"))]
     device = torch.device("cuda" if device is None else device)
     index = torch.cuda.current_device() if device.index is None else device.index
-    return _linear_workspace(int(T), int(B), int(H), int(backward), index)
+    return _linear_workspace(*sizes, index)
 
 
 class Q4Matrix:
@@ -556,8 +567,9 @@ def approx_lstm_q4_prepare(w, group=128, stream=None):
     if w.ndim != 2:
         raise ValueError(f"w has shape {w.shape}, expected (rows, cols)")
     out = ctypes.c_void_p()
-    _check(lib.approx_lstm_q4_prepare(wp, *w.shape, int(group), _stream(stream), ctypes.byref(out)))
-    return Q4Matrix(out.value, *w.shape, int(group), torch.cuda.current_device())
+    rows, cols, group = _int32(w.shape[0], "rows"), _int32(w.shape[1], "cols"), _int32(int(group), "group")
+    _check(lib.approx_lstm_q4_prepare(wp, rows, cols, group, _stream(stream), ctypes.byref(out)))
+    return Q4Matrix(out.value, rows, cols, group, torch.cuda.current_device())
 
 
 def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):
@@ -566,8 +578,8 @@ def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):
     (None: 8): GPU tensors; returns a Q4Matrix."""
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 2:
         raise TypeError("q must be a torch tensor [rows, ceil(cols / 2)] on the GPU")
-    cols, group, index = int(cols), int(group), q.get_device()
-    rows, groups = q.shape[0], -(-cols // group) if group > 0 else 0
+    cols, group, index = _int32(int(cols), "cols"), _int32(int(group), "group"), q.get_device()
+    rows, groups = _int32(q.shape[0], "rows"), -(-cols // group) if group > 0 else 0
     out = ctypes.c_void_p()
     at = (_on(q, "q", (rows, (cols + 1) // 2), torch.uint8, index),
           _on(scale, "scale", (rows, groups), torch.float32, index),
@@ -595,7 +607,7 @@ def approx_lstm_q4_run(m, x, y, bias=None, stream=None):
         raise TypeError("x must be a torch tensor [N, cols] on the GPU")
     if x.dtype not in _DTYPES:
         raise TypeError("x must be float32 or bfloat16")
-    N, at = x.shape[0], m.device
+    N, at = _int32(x.shape[0], "N"), m.device
     args = (m.handle, _on(x, "x", (N, m.cols), x.dtype, at), N, _DTYPES[x.dtype],
             None if bias is None else _on(bias, "bias", (m.rows,), torch.float32, at),
             _on(y, "y", (N, m.rows), x.dtype, at))

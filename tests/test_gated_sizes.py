@@ -3,7 +3,9 @@ anything is computed from them, by the workspace query as by the calls (no GPU).
 
 import ctypes
 
+import numpy as np
 import pytest
+import torch
 
 from paper_1905_00689_amd import binding as B
 
@@ -34,3 +36,26 @@ def test_backward_passes_of_too_many_pieces(T, Bn, H):
     for backward in (1, 2):
         assert query(T, Bn, H, backward) == (6, 77)
     assert B.lib.approx_lstm_linear_backward(P, None, T, Bn, H, 1, None, P, P, None, P, None, P, None, 0, None) == 6
+
+
+def test_sizes_of_more_than_32_bits_are_not_cut():
+    """2^32 + 5 timesteps are not five."""
+    for T, Bn, H in (((1 << 32) + 5, 1, 64), (5, (1 << 32) + 1, 64), (5, 1, (1 << 32) + 64), (1 << 31, 1, 1)):
+        with pytest.raises(ValueError):
+            B.approx_lstm_linear_workspace(T, Bn, H, 0, "cuda:0")
+    assert B._int32((1 << 31) - 1, "n") == (1 << 31) - 1
+
+
+@pytest.mark.gpu
+def test_tensors_of_more_than_2_32_rows_are_refused():
+    n = 1 << 32
+    p, h = torch.empty(n + 5, 1, 4, dtype=torch.bfloat16, device="cuda"), torch.empty(n + 5, 1, 1, dtype=torch.bfloat16,
+                                                                                      device="cuda")
+    with pytest.raises(ValueError):
+        B.approx_lstm_linear_run(p, h)
+    with pytest.raises(ValueError):   # as many sequences
+        B.approx_lstm_linear_run(p.view(1, n + 5, 4), h.view(1, n + 5, 1))
+    del p
+    m = B.approx_lstm_q4_prepare(np.ones((1, 1), np.float32), 32)
+    with pytest.raises(ValueError):
+        B.approx_lstm_q4_run(m, h.view(n + 5, 1), torch.empty_like(h).view(n + 5, 1))
