@@ -481,8 +481,8 @@ def _linear_call(function, T, B, H, backward, index, workspace, stream, args):
     def call(s):
         if s == _raw_stream(index):
             ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{index}")
-        else:   # from the pool of the stream that uses it
-            with torch.cuda.stream(torch.cuda.ExternalStream(s, device=index)):
+        else:   # from the pool of the stream that uses it (a handle of 0 would make ExternalStream a stream of its own)
+            with torch.cuda.stream(torch.cuda.ExternalStream(s, device=index) if s else torch.cuda.default_stream(index)):
                 ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{index}")
         return function(*args, ws.data_ptr(), n, s)
 
