@@ -132,9 +132,11 @@ __device__ __forceinline__ Lane lane_of(const LinearArgs& a, int idx) {
   return l;
 }
 
-// Gates with the bias inside the exponential's argument: sigmoid(x + b) = 1 / (1 +
-// 2^(k x + k b)), k = -log2 e, and tanh(x + b) = 1 - 2 / (1 + 2^(-2 k (x + b))).
-// Both reach their ends exactly (2^x is 0 or infinity there).
+// Gates of y = p + bias, rounded once: a bias inside the exponential's argument (one
+// operation less) would be rounded apart from p, and what is left where the two
+// cancel would be off by as much as they are.  sigmoid(y) = 1 / (1 + 2^(-y log2 e)) and
+// tanh(y) = 1 - 2 / (1 + 2^(2 y log2 e)) reach their ends exactly (2^x is 0 or infinity
+// there).
 struct GateBias {
   f32x2 i, f, g, o;
 };
@@ -144,26 +146,29 @@ __device__ __forceinline__ GateBias gate_bias(const LinearArgs& a, const Lane& l
   if (a.bias) {
     auto at = [&](int q) {
       const float* p = a.bias + (size_t)q * a.H + l.r;
-      return f32x2{p[0], p[l.two ? 1 : 0]};
+      float lo = p[0], hi = p[l.two ? 1 : 0];
+      // (arrived before anything else is under way: waits at their uses would be for the
+      // stores of h as well, T = 100, H = 64, fp32 10.2 us instead of 9.0)
+      asm("" : "+v"(lo), "+v"(hi));
+      return f32x2{lo, hi};
     };
-    b.i = at(0) * -kLog2e, b.f = at(1) * -kLog2e, b.g = at(2) * (2.0f * kLog2e), b.o = at(3) * -kLog2e;
+    b.i = at(0), b.f = at(1), b.g = at(2), b.o = at(3);
   }
   return b;
 }
 
-__device__ __forceinline__ float gate_sig(float x, float b) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, -kLog2e, b)));
+__device__ __forceinline__ float gate_sig(float y) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * -kLog2e));
 }
 // The forget gate: over a memory of 1 / (1 - f) steps an error of the same sign in
 // each adds up, and the reciprocal's is (0.1 of half a step on average at f near 1;
 // 0.006 after one Newton step).  fminf keeps 0 x infinity out where the gate is shut.
-__device__ __forceinline__ float gate_forget(float x, float b) {
-  const float d = 1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, -kLog2e, b)), r = __builtin_amdgcn_rcpf(d);
+__device__ __forceinline__ float gate_forget(float y) {
+  const float d = 1.0f + __builtin_amdgcn_exp2f(y * -kLog2e), r = __builtin_amdgcn_rcpf(d);
   return __builtin_fmaf(fminf(__builtin_fmaf(-r, d, 1.0f), 1e-6f), r, r);
 }
-__device__ __forceinline__ float gate_tanh(float x, float b) {
-  return __builtin_fmaf(
-      -2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(__builtin_fmaf(x, 2.0f * kLog2e, b))), 1.0f);
+__device__ __forceinline__ float gate_tanh(float y) {
+  return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * (2.0f * kLog2e))), 1.0f);
 }
 
 // Few timesteps: a lane walks its two units through all of them, the loads of
@@ -198,8 +203,8 @@ __global__ void __launch_bounds__(kWalkThreads) linear_walk_kernel(LinearArgs a)
       if (t < l.len) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          c[k] = __builtin_fmaf(gate_forget(yf[k], bias.f[k]), c[k], gate_sig(yi[k], bias.i[k]) * gate_tanh(yg[k], bias.g[k]));
-          h[k] = gate_sig(yo[k], bias.o[k]) * gate_tanh(c[k], 0.f);
+          c[k] = __builtin_fmaf(gate_forget(yf[k] + bias.f[k]), c[k], gate_sig(yi[k] + bias.i[k]) * gate_tanh(yg[k] + bias.g[k]));
+          h[k] = gate_sig(yo[k] + bias.o[k]) * gate_tanh(c[k]);
         }
       }
       store_pair<T, R>((char*)a.h + (size_t)t * (BH * sizeof(T)), l.at * sizeof(T), h, l.two);
@@ -390,8 +395,8 @@ __global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T)
         const f32x2 yi = Pair<T>::get(raw[k][0]), yf = Pair<T>::get(raw[k][1]), yg = Pair<T>::get(raw[k][2]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          f[k][j] = gate_forget(yf[j], bias.f[j]);
-          u[k][j] = gate_sig(yi[j], bias.i[j]) * gate_tanh(yg[j], bias.g[j]);
+          f[k][j] = gate_forget(yf[j] + bias.f[j]);
+          u[k][j] = gate_sig(yi[j] + bias.i[j]) * gate_tanh(yg[j] + bias.g[j]);
         }
       }
     }
@@ -426,7 +431,7 @@ __global__ void __launch_bounds__(kScanThreads, LOOK && !(R == kOdd && sizeof(T)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           c[j] = __builtin_fmaf(f[k][j], c[j], u[k][j]);
-          h[j] = gate_sig(yo[j], bias.o[j]) * gate_tanh(c[j], 0.f);
+          h[j] = gate_sig(yo[j] + bias.o[j]) * gate_tanh(c[j]);
           if (k >= n) h[j] = 0.f;
         }
         if (t0 + k < a.T) store_pair<T, R>((char*)a.h + (size_t)(t0 + k) * (BH * sizeof(T)), ha, h, l.two);
@@ -492,12 +497,12 @@ __global__ void __launch_bounds__(64 * W, 4) linear_back_kernel(LinearArgs a, Li
     f32x2 dO;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float vf = gate_forget(yf[j], bias.f[j]), vi = gate_sig(yi[j], bias.i[j]), vg = gate_tanh(yg[j], bias.g[j]),
-                  vo = gate_sig(yo[j], bias.o[j]);
+      const float vf = gate_forget(yf[j] + bias.f[j]), vi = gate_sig(yi[j] + bias.i[j]), vg = gate_tanh(yg[j] + bias.g[j]),
+                  vo = gate_sig(yo[j] + bias.o[j]);
       kf[k][j] = c[j] * __builtin_fmaf(-vf, vf, vf);
       ki[k][j] = vg * __builtin_fmaf(-vi, vi, vi);
       kg[k][j] = vi * __builtin_fmaf(-vg, vg, 1.f);
-      const float cn = __builtin_fmaf(vf, c[j], vi * vg), tc = gate_tanh(cn, 0.f), dho = dh[j] * vo;
+      const float cn = __builtin_fmaf(vf, c[j], vi * vg), tc = gate_tanh(cn), dho = dh[j] * vo;
       f[k][j] = vf;
       w[k][j] = dho * __builtin_fmaf(-tc, tc, 1.f);
       dO[j] = dho * tc * (1.f - vo);
