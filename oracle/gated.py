@@ -93,6 +93,54 @@ def linear_lstm_grad(p, dh, dc_out=None, bias=None, lengths=None, c0=None):
     return dict(dp=dp.reshape(T, B, H4), dc0=e, dbias=db), dict(dp=bd.reshape(T, B, H4), dc0=err, dbias=db_err)
 
 
+def linear_lstm_small(p, dh, dc_out=None, bias=None, lengths=None, c0=None):
+    """Bounds dict(h, c, dp, dc0) on fp32 errors that small values keep relative to
+    themselves: nothing in them is a multiple of u alone.
+
+    In units of u: y = p + bias is off by |y|, 2^(y log2 e) by 2.25 |y| (the sum, the
+    product, the constant) and 2 (the exponential) of itself, so a sigmoid s by
+    S = 3 + (1 - s)(2.25 |y| + 2) of itself (the sum 1, the reciprocal 2).  A tanh is off
+    by 8 of itself (an odd series near 0, 1 - 2 / (1 + e^2y) elsewhere) and its argument's
+    error.  f c adds S + 1, i g S + 10, and 3 of each for the roundings of a step and of
+    the maps that join pieces of time.  The rest is the same a product at a time.
+    """
+    T, B, H4 = p.shape
+    H = H4 // 4
+    i, f, g, o = _gates(p, bias)
+    y = np.abs(p.astype(np.float64) + (0.0 if bias is None else bias.astype(np.float64)))
+    Si, Sf, So = (3 + (1 - s) * (2.25 * y[..., k * H:(k + 1) * H] + 2) for s, k in ((i, 0), (f, 1), (o, 3)))
+    _, c, _, _ = linear_lstm(p, bias, lengths, c0)
+    live = _live(T, B, lengths)[..., None]
+    env, err = np.abs(c), np.zeros_like(c)
+    for t in range(T):
+        fc, ig = f[t] * env[t], np.abs(i[t] * g[t])
+        env[t + 1] = np.where(live[t], fc + ig, env[t])
+        err[t + 1] = np.where(live[t], f[t] * err[t] + U32 * (fc * (Sf[t] + 4) + ig * (Si[t] + 13)), err[t])
+    th = np.abs(np.tanh(c[1:]))
+    terr = err[1:] + 8 * U32 * th
+    h = np.where(live, o * terr + U32 * o * th * (So + 1), 0.0)
+    dh = np.where(live, np.abs(dh.astype(np.float64)), 0.0)
+    env_e = np.zeros((B, H)) if dc_out is None else np.abs(dc_out.astype(np.float64))
+    err_e, dp = np.zeros((B, H)), np.zeros((T, B, 4, H))
+    a, up = np.abs(c), 1 - th ** 2
+    for t in range(T - 1, -1, -1):
+        de = dh[t] * o[t] * up[t] + env_e
+        derr = dh[t] * o[t] * (up[t] * (So[t] + 3) * U32 + 2 * th[t] * terr[t]) + err_e + U32 * de
+        i1, f1, g1, o1 = i[t] * (1 - i[t]), f[t] * (1 - f[t]), 1 - g[t] ** 2, o[t] * (1 - o[t])
+        gi, gf = i[t] * np.abs(1 - 2 * i[t]) * Si[t], f[t] * np.abs(1 - 2 * f[t]) * Sf[t]
+        ag = np.abs(g[t])
+        dp[t] = np.stack([
+            derr * ag * i1 + de * ag * U32 * (gi + 12 * i1),
+            derr * a[t] * f1 + de * (a[t] * U32 * (gf + 3 * f1) + err[t] * f1),
+            derr * i[t] * g1 + de * i[t] * U32 * (g1 * (Si[t] + 3) + 18 * g[t] ** 2),
+            dh[t] * (o1 * (terr[t] + th[t] * (So[t] + 4) * U32) + th[t] * o[t] ** 2 * So[t] * U32)], 1)
+        lv = live[t]
+        dp[t] *= lv[:, None]
+        err_e = np.where(lv, f[t] * derr + U32 * f[t] * de * (Sf[t] + 5), err_e)
+        env_e = np.where(lv, f[t] * de, env_e)
+    return dict(h=h, c=err, dp=dp.reshape(T, B, H4), dc0=err_e)
+
+
 def q4_round(w, group):
     """Levels q [R, D], scale and zero [R, groups] of a float32 matrix."""
     R, D = w.shape

@@ -2,15 +2,18 @@
 added to p before anything is made of the sum, and what is small is good
 relative to itself, forward and back."""
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import gated
 from paper_1905_00689_amd import binding as B
 
 from .gpu_helpers import say
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
 
 
 def passes(p, dh, dc, c0, bias, lengths=None):
@@ -41,3 +44,36 @@ def test_a_bias_that_cancels_leaves_nothing_behind(T, Bn, H, dtype):
     want = passes(v.to(dtype).cuda(), dh.to(dtype), dc, c0, None)
     for name in want:
         assert torch.equal(got[name], want[name]), name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("ragged", [False, True], ids=["", "ragged"])
+@pytest.mark.parametrize("T,Bn,H", [(1, 3, 64), (12, 2, 33), (100, 2, 64), (700, 2, 65)])
+def test_small_candidates_and_states_are_good_relative_to_themselves(T, Bn, H, ragged, dtype):
+    """Candidates g and states c of 1e-7 to 1, a magnitude to a unit: h, c and
+    the gradients against float64 within bounds relative to what they are made of."""
+    say("small", T, Bn, H, ragged, dtype)
+    r = np.random.default_rng([190500689, 77, T, H])
+    size = 10.0 ** (-7 + 7 * np.arange(H) / H)
+    p = r.normal(size=(T, Bn, 4, H))
+    p[:, :, 0] *= 2
+    p[:, :, 1] += 1
+    p[:, :, 2] *= size
+    bias = r.normal(size=(4, H))
+    bias[2] *= size
+    t = lambda a, d=F32: torch.from_numpy(a).to(d).cuda()  # noqa: E731
+    p, bias = t(p.reshape(T, Bn, 4 * H), dtype), t(bias.reshape(4 * H))
+    c0, dh, dc = t(r.normal(size=(Bn, H)) * size), t(r.normal(size=(T, Bn, H)), dtype), t(r.normal(size=(Bn, H)))
+    lengths = torch.tensor([T, 2 * T // 3, 0][:Bn], dtype=torch.int32, device="cuda") if ragged else None
+    got = passes(p, dh, dc, c0, bias, lengths)
+    host = lambda a: None if a is None else a.double().cpu().numpy()  # noqa: E731
+    n = None if lengths is None else lengths.cpu().numpy()
+    h, c, _, _ = gated.linear_lstm(host(p), host(bias), n, host(c0))
+    g, _ = gated.linear_lstm_grad(host(p), host(dh), host(dc), host(bias), n, host(c0))
+    bound = gated.linear_lstm_small(host(p), host(dh), host(dc), host(bias), n, host(c0))
+    for name, want, b, half in (("h", h, bound["h"], HALF[dtype]), ("c", c[-1], bound["c"][-1], HALF[F32]),
+                                ("save", c[:-1][::8], bound["c"][:-1][::8], HALF[F32]),
+                                ("dp", g["dp"], bound["dp"], HALF[dtype]), ("dc0", g["dc0"], bound["dc0"], HALF[F32])):
+        worst = np.max(np.abs(host(got[name]) - want) / (b * (1 + half) + half * np.abs(want) + 1e-30))
+        say(name, "worst share of the tolerance %.2f" % worst)
+        assert np.isfinite(host(got[name])).all() and worst <= 1.0, (name, worst)
