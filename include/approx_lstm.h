@@ -586,7 +586,14 @@ approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H,
  * Asynchronous on hip_stream, allocates nothing, can be captured; a matrix is
  * never written by a run, so runs may overlap.  x and y must not overlap.
  *
- * Errors: INVALID_ARG for a null m, x or y, sizes below those above, another
+ * approx_lstm_q4_plan -- the kernel that a run over N rows of x takes, without any
+ * device work (for tests and tuning): num_cu compute units to plan for (0: the
+ * current device's), out host [4]: 0 dot, 1 row or 2 tile kernel, its row tiles of 16
+ * a workgroup (of a wave in the tile kernel), its rows of x (dot kernel) or 16s of them,
+ * and the waves, or halves of the columns (tile kernel), that share the columns.  Of
+ * more than 2^20 rows of x, that of each launch but the last.
+ *
+ * Errors: INVALID_ARG for a null m, x, y or out, sizes below those above, another
  * dtype or group, a pointer not aligned to its elements, weights that are not
  * finite, a zero level above 15.
  */
@@ -600,6 +607,8 @@ approx_lstm_status approx_lstm_q4_get(const approx_lstm_q4* m, uint8_t* q, float
                                       void* hip_stream);
 approx_lstm_status approx_lstm_q4_run(const approx_lstm_q4* m, const void* x, int32_t N, int32_t dtype,
                                       const float* bias, void* y, void* hip_stream);
+approx_lstm_status approx_lstm_q4_plan(int32_t rows, int32_t cols, int32_t group, int32_t N, int32_t dtype, int32_t num_cu,
+                                       int32_t* out);
 void approx_lstm_q4_destroy(approx_lstm_q4* m);
 
 /* approx_lstm_destroy -- free the model and its device memory (NULL is a no-op). */

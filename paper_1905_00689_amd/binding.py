@@ -96,6 +96,7 @@ _sigs.update({
     "approx_lstm_q4_load": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, ctypes.POINTER(_vp)],
     "approx_lstm_q4_get": [_vp, _vp, _vp, _vp, _vp],
     "approx_lstm_q4_run": [_vp, _vp, _i32, _i32, _vp, _vp, _vp],
+    "approx_lstm_q4_plan": [_i32, _i32, _i32, _i32, _i32, _i32, _vp],
 })
 for _name, _args in _sigs.items():
     getattr(lib, _name).argtypes = _args
@@ -612,3 +613,12 @@ def approx_lstm_q4_run(m, x, y, bias=None, stream=None):
             None if bias is None else _on(bias, "bias", (m.rows,), torch.float32, at),
             _on(y, "y", (N, m.rows), x.dtype, at))
     return _launch(at, stream, lambda s: lib.approx_lstm_q4_run(*args, s))
+
+
+def approx_lstm_q4_plan(rows, cols, group, N, dtype=torch.float32, num_cu=0):
+    """The kernel that a product with N rows of x takes (no device work where num_cu is
+    given): ("dot", "rows" or "tile", its row tiles, its rows of x, its split)."""
+    out = np.zeros(4, np.int32)
+    sizes = [_int32(int(v), name) for v, name in ((rows, "rows"), (cols, "cols"), (group, "group"), (N, "N"))]
+    _check(lib.approx_lstm_q4_plan(*sizes, _DTYPES[dtype], int(num_cu), out.ctypes.data))
+    return (("dot", "rows", "tile")[out[0]], *(int(v) for v in out[1:]))

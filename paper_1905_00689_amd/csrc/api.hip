@@ -1741,6 +1741,15 @@ approx_lstm_status check_linear(alstm::LinearArgs& a, int dtype, int backward, c
   return APPROX_LSTM_OK;
 }
 
+approx_lstm_status check_q4_sizes(int rows, int cols, int group) {
+  if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (rows > 1 << 25 || cols > 1 << 30)
+    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "more than 2^25 rows or 2^30 columns");
+  if (group != 32 && group != 64 && group != 128)
+    return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
+  return APPROX_LSTM_OK;
+}
+
 }  // namespace
 
 struct approx_lstm_q4 {
@@ -1809,16 +1818,12 @@ approx_lstm_status approx_lstm_q4_load(const uint8_t* q, const float* scale, con
                                        int32_t cols, int32_t group, void* hip_stream, approx_lstm_q4** out) {
   g_last_error.clear();
   if (!q || !scale || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
-  if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
-  if (rows > 1 << 25 || cols > 1 << 30)
-    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "more than 2^25 rows or 2^30 columns");
-  if (group != 32 && group != 64 && group != 128)
-    return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
+  approx_lstm_status st = check_q4_sizes(rows, cols, group);
+  if (st != APPROX_LSTM_OK) return st;
   if (!aligned(scale, 4)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "scale not aligned to 4 bytes");
   approx_lstm_q4* m = new (std::nothrow) approx_lstm_q4();
   if (!m) return fail(APPROX_LSTM_ERR_OUT_OF_MEMORY, "host allocation failed");
   hipStream_t stream = (hipStream_t)hip_stream;
-  approx_lstm_status st = APPROX_LSTM_OK;
   auto step = [&](hipError_t e, const char* what) {
     if (st == APPROX_LSTM_OK && e != hipSuccess) st = hip_fail(e, what);
   };
@@ -1849,11 +1854,8 @@ approx_lstm_status approx_lstm_q4_prepare(const float* w, int32_t rows, int32_t 
                                           void* hip_stream, approx_lstm_q4** out) {
   g_last_error.clear();
   if (!w || !out) return fail(APPROX_LSTM_ERR_INVALID_ARG, "null pointer argument");
-  if (rows < 1 || cols < 1) return fail(APPROX_LSTM_ERR_INVALID_ARG, "sizes must be >= 1");
-  if (rows > 1 << 25 || cols > 1 << 30)
-    return fail(APPROX_LSTM_ERR_UNSUPPORTED, "more than 2^25 rows or 2^30 columns");
-  if (group != 32 && group != 64 && group != 128)
-    return fail(APPROX_LSTM_ERR_INVALID_ARG, "group = %d is not 32, 64 or 128", group);
+  approx_lstm_status st = check_q4_sizes(rows, cols, group);
+  if (st != APPROX_LSTM_OK) return st;
   const size_t R = rows, D = cols, groups = (D + group - 1) / group, row_bytes = (D + 1) / 2;
   std::vector<uint8_t> q, z;
   std::vector<float> s;
@@ -1888,7 +1890,6 @@ approx_lstm_status approx_lstm_q4_prepare(const float* w, int32_t rows, int32_t 
   uint8_t* d_q = nullptr;
   float* d_s = nullptr;
   uint8_t* d_z = nullptr;
-  approx_lstm_status st = APPROX_LSTM_OK;
   auto step = [&](hipError_t e, const char* what) {
     if (st == APPROX_LSTM_OK && e != hipSuccess) st = hip_fail(e, what);
   };
@@ -1949,6 +1950,20 @@ approx_lstm_status approx_lstm_q4_run(const approx_lstm_q4* m, const void* x, in
   DeviceScope ds(m->device);
   if (!ds.ok) return fail(APPROX_LSTM_ERR_DEVICE, "cannot select the matrix's device");
   HIP_TRY(alstm::launch_q4(m->m, x, N, dtype, bias, y, m->num_cu, (hipStream_t)hip_stream), "launch q4 product");
+  return APPROX_LSTM_OK;
+}
+
+approx_lstm_status approx_lstm_q4_plan(int32_t rows, int32_t cols, int32_t group, int32_t N, int32_t dtype, int32_t num_cu,
+                                       int32_t* out) {
+  g_last_error.clear();
+  if (!out || N < 1 || num_cu < 0 || (dtype != 0 && dtype != 1)) return fail(APPROX_LSTM_ERR_INVALID_ARG, "bad arguments");
+  approx_lstm_status st = check_q4_sizes(rows, cols, group);
+  if (st == APPROX_LSTM_OK && num_cu == 0) st = current_cus(&num_cu);
+  if (st != APPROX_LSTM_OK) return st;
+  alstm::Q4Matrix m{};
+  alstm::q4_shape(m, rows, cols, group);
+  const alstm::Q4Form f = alstm::q4_form(m, std::min(N, alstm::kQ4MostRows), dtype, num_cu);
+  out[0] = f.kernel, out[1] = f.tiles, out[2] = f.x, out[3] = f.split;
   return APPROX_LSTM_OK;
 }
 

@@ -71,6 +71,16 @@ hipError_t launch_q4_layout(const Q4Matrix& m, const uint8_t* q, const float* sc
                             hipStream_t stream);
 // The opposite: the matrix in the formats of its layout's arguments.
 hipError_t launch_q4_unpack(const Q4Matrix& m, uint8_t* q, float* scale, uint8_t* zero, hipStream_t stream);
+// The kernel of a product and its shape: row tiles of a workgroup (of a wave in the
+// tile kernel), rows of x (dot) or 16s of them, and waves, or halves of the columns
+// (tile), that share the columns.
+enum Q4Kernel { kQ4Dot, kQ4Rows, kQ4Tile };
+struct Q4Form {
+  Q4Kernel kernel;
+  int tiles, x, split;
+};
+Q4Form q4_form(const Q4Matrix& m, int N, int bf16, int num_cu);
+constexpr int kQ4MostRows = 1 << 20;   // of x in a launch (a grid's second dimension is short)
 // y [N][R] = x [N][D] times the matrix, plus bias [R] (or null).
 hipError_t launch_q4(const Q4Matrix& m, const void* x, int N, int bf16, const float* bias, void* y, int num_cu,
                      hipStream_t stream);

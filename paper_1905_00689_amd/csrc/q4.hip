@@ -620,48 +620,68 @@ void launch_dot(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, h
 
 template <class T, int G>
 void launch_group(const Q4Matrix& m, const T* x, int N, const float* bias, T* y, int num_cu, hipStream_t stream) {
-  // What both sides took, in us, D = 2048 unless given:
-  // - many rows of x: the tile kernel once half the compute units get a workgroup of it;
-  //   64 rows of x at a time where that makes two a unit (bf16, 4096 x 2048: 49, 32 at a
-  //   time 54; 2048 x 2048: 36 and 31), in fp32 always 32 (8192 x 2048: 211, 64 at a time
-  //   254 with spilled registers); the columns in two halves where there is at most a
-  //   workgroup a unit (R = 2048, N = 1024, bf16 19, whole 23, fp32 34 and 40; R = 3716, D =
-  //   2951, N = 730, 345 workgroups: 52 and 45).  Row kernel / tile kernel: R = 2048, N =
-  //   256, bf16 9 / 18, fp32 15 / 31; N = 512 16.5 / 18.7, 46 / 31; N = 1024 42 / 19, 89 / 34;
-  //   R = 256, D = 4096, N = 4096 50 / 36, 76 / 63.
-  // - one row, in fp32 two: the dot kernel (fp32, G = 32, R = 32768, D = 8192: 40, row
-  //   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
-  //   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
-  //   D = 8256: 8.4, eight waves 14).
-  // - else the row kernel, in the widest shape that still has a workgroup a unit: fp32,
-  //   R = 8192, N = 12: 32 x 16 7.2, 64 x 16 10.4; N = 48 64 x 32 15, 32 x 64 19; R = 256,
-  //   D = 8256, N = 100: 16 x 16 23, 32 x 64 87.  Below that 16 x 16 on sixteen waves, but
-  //   32 x 32 once they do not all run at once (bf16, G = 32, R = 1000, D = 2000, N = 200:
-  //   13 and 7.8; R = 2048, D = 4096, N = 64, two a unit: 10.4 and 11.9).
-  const size_t tiles = m.tiles, cu = num_cu;
-  auto cover = [](size_t n, size_t by) { return (n + by - 1) / by; };
   constexpr bool kHalf = sizeof(T) == 2;
-  const size_t wide = cover(m.R, kTileRows) * cover(N, 64), narrow = cover(m.R, kTileRows) * cover(N, 32);
-  if constexpr (kHalf)
-    if (N > 64 && wide >= 2 * cu) return launch_tile<T, G, 4, 1>(m, x, N, bias, y, stream);
-  if (N > 64 && narrow > cu) launch_tile<T, G, 2, 1>(m, x, N, bias, y, stream);
-  else if (N > 64 && 2 * narrow >= cu) launch_tile<T, G, 2, 2>(m, x, N, bias, y, stream);
-  else if (N == 1 && tiles >= 4 * cu) launch_dot<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
-  else if (N == 1 && tiles >= 2 * cu) launch_dot<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
-  else if (N == 1) launch_dot<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
-  else if (N == 2 && !kHalf && tiles >= 2 * cu) launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
-  else if (N == 2 && !kHalf) launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
-  else if (N <= 16 && tiles >= 4 * cu) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
-  else if (N <= 16 && tiles >= 2 * cu) launch_rows<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
-  else if (N > 16 && cover(tiles, 4) * cover(N, 32) >= cu) launch_rows<T, G, 4, 2, 8>(m, x, N, bias, y, stream);
-  else if (N > 16 && (cover(tiles, 2) * cover(N, 32) >= cu || tiles * cover(N, 16) > 2 * cu))
-    launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+  const Q4Form f = q4_form(m, N, kHalf, num_cu);
+  auto is = [&](Q4Kernel k, int tiles, int x_rows, int split) {
+    return f.kernel == k && f.tiles == tiles && f.x == x_rows && f.split == split;
+  };
+  if constexpr (kHalf) {
+    if (is(kQ4Tile, 4, 4, 1)) return launch_tile<T, G, 4, 1>(m, x, N, bias, y, stream);
+  } else {
+    if (is(kQ4Dot, 2, 2, 8)) return launch_dot<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
+    if (is(kQ4Dot, 1, 2, 16)) return launch_dot<T, G, 1, 2, 16>(m, x, N, bias, y, stream);
+  }
+  if (is(kQ4Tile, 4, 2, 1)) launch_tile<T, G, 2, 1>(m, x, N, bias, y, stream);
+  else if (is(kQ4Tile, 4, 2, 2)) launch_tile<T, G, 2, 2>(m, x, N, bias, y, stream);
+  else if (is(kQ4Dot, 4, 1, 8)) launch_dot<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
+  else if (is(kQ4Dot, 2, 1, 8)) launch_dot<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
+  else if (is(kQ4Dot, 1, 1, 16)) launch_dot<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
+  else if (is(kQ4Rows, 4, 1, 8)) launch_rows<T, G, 4, 1, 8>(m, x, N, bias, y, stream);
+  else if (is(kQ4Rows, 2, 1, 8)) launch_rows<T, G, 2, 1, 8>(m, x, N, bias, y, stream);
+  else if (is(kQ4Rows, 4, 2, 8)) launch_rows<T, G, 4, 2, 8>(m, x, N, bias, y, stream);
+  else if (is(kQ4Rows, 2, 2, 8)) launch_rows<T, G, 2, 2, 8>(m, x, N, bias, y, stream);
   else launch_rows<T, G, 1, 1, 16>(m, x, N, bias, y, stream);
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
+
+// What both sides took, in us, D = 2048 unless given:
+// - many rows of x: the tile kernel once half the compute units get a workgroup of it;
+//   64 rows of x at a time where that makes two a unit (bf16, 4096 x 2048: 49, 32 at a
+//   time 54; 2048 x 2048: 36 and 31), in fp32 always 32 (8192 x 2048: 211, 64 at a time
+//   254 with spilled registers); the columns in two halves where there is at most a
+//   workgroup a unit (R = 2048, N = 1024, bf16 19, whole 23, fp32 34 and 40; R = 3716, D =
+//   2951, N = 730, 345 workgroups: 52 and 45).  Row kernel / tile kernel: R = 2048, N =
+//   256, bf16 9 / 18, fp32 15 / 31; N = 512 16.5 / 18.7, 46 / 31; N = 1024 42 / 19, 89 / 34;
+//   R = 256, D = 4096, N = 4096 50 / 36, 76 / 63.
+// - one row, in fp32 two: the dot kernel (fp32, G = 32, R = 32768, D = 8192: 40, row
+//   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
+//   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
+//   D = 8256: 8.4, eight waves 14).
+// - else the row kernel, in the widest shape that still has a workgroup a unit: fp32,
+//   R = 8192, N = 12: 32 x 16 7.2, 64 x 16 10.4; N = 48 64 x 32 15, 32 x 64 19; R = 256,
+//   D = 8256, N = 100: 16 x 16 23, 32 x 64 87.  Below that 16 x 16 on sixteen waves, but
+//   32 x 32 once they do not all run at once (bf16, G = 32, R = 1000, D = 2000, N = 200:
+//   13 and 7.8; R = 2048, D = 4096, N = 64, two a unit: 10.4 and 11.9).
+Q4Form q4_form(const Q4Matrix& m, int N, int bf16, int num_cu) {
+  const size_t tiles = m.tiles, cu = num_cu;
+  auto cover = [](size_t n, size_t by) { return (n + by - 1) / by; };
+  const size_t wide = cover(m.R, kTileRows) * cover(N, 64), narrow = cover(m.R, kTileRows) * cover(N, 32);
+  if (N > 64 && bf16 && wide >= 2 * cu) return {kQ4Tile, 4, 4, 1};
+  if (N > 64 && narrow > cu) return {kQ4Tile, 4, 2, 1};
+  if (N > 64 && 2 * narrow >= cu) return {kQ4Tile, 4, 2, 2};
+  if (N == 1 && tiles >= 4 * cu) return {kQ4Dot, 4, 1, 8};
+  if (N == 1 && tiles >= 2 * cu) return {kQ4Dot, 2, 1, 8};
+  if (N == 1) return {kQ4Dot, 1, 1, 16};
+  if (N == 2 && !bf16) return tiles >= 2 * cu ? Q4Form{kQ4Dot, 2, 2, 8} : Q4Form{kQ4Dot, 1, 2, 16};
+  if (N <= 16 && tiles >= 4 * cu) return {kQ4Rows, 4, 1, 8};
+  if (N <= 16 && tiles >= 2 * cu) return {kQ4Rows, 2, 1, 8};
+  if (N > 16 && cover(tiles, 4) * cover(N, 32) >= cu) return {kQ4Rows, 4, 2, 8};
+  if (N > 16 && (cover(tiles, 2) * cover(N, 32) >= cu || tiles * cover(N, 16) > 2 * cu)) return {kQ4Rows, 2, 2, 8};
+  return {kQ4Rows, 1, 1, 16};
+}
 
 void q4_shape(Q4Matrix& m, int R, int D, int G) {
   m.R = R, m.D = D, m.G = G;
@@ -697,11 +717,10 @@ hipError_t launch_q4_unpack(const Q4Matrix& m, uint8_t* q, float* scale, uint8_t
 
 hipError_t launch_q4(const Q4Matrix& m, const void* x, int N, int bf16, const float* bias, void* y, int num_cu,
                      hipStream_t stream) {
-  constexpr int kMostRows = 1 << 20;   // of a launch (a grid's second dimension is short)
   auto go = [&](auto g) {
     constexpr int G = decltype(g)::value;
-    for (int n = 0; n < N; n += std::min(N - n, kMostRows)) {
-      const int c = std::min(N - n, kMostRows);
+    for (int n = 0; n < N; n += std::min(N - n, kQ4MostRows)) {
+      const int c = std::min(N - n, kQ4MostRows);
       const size_t in = (size_t)n * m.D, out = (size_t)n * m.R;
       if (bf16) launch_group<__bf16, G>(m, (const __bf16*)x + in, c, bias, (__bf16*)y + out, num_cu, stream);
       else launch_group<float, G>(m, (const float*)x + in, c, bias, (float*)y + out, num_cu, stream);

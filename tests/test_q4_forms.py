@@ -1,0 +1,59 @@
+"""The rule between the kernels of the 4-bit products, and what the measures of
+their errors see (no GPU)."""
+
+import numpy as np
+import pytest
+
+from oracle import gated
+from paper_1905_00689_amd import binding as B
+
+from .q4_cases import ALL, BF16, F32, FORMS, IDS, levels, one_column, one_column_share, rms_share
+
+
+@pytest.mark.parametrize("form,dtype", ALL, ids=IDS)
+def test_every_kernel_has_its_case(form, dtype):
+    N, R, widths = FORMS[form]
+    for G in (32, 64, 128):
+        for D in widths:
+            assert B.approx_lstm_q4_plan(R, D, G, N, dtype, 256) == form
+
+
+def test_the_rule_knows_no_other_kernel():
+    r = np.random.default_rng(5)
+    seen = set()
+    for _ in range(20000):
+        N, R, D = (int(2 ** r.uniform(0, e)) for e in (21, 17, 14))
+        cu, dtype = int(r.choice([1, 64, 256, 304])), (F32, BF16)[int(r.integers(2))]
+        form = B.approx_lstm_q4_plan(R, D, 64, N, dtype, cu)
+        assert (form, dtype) in ALL
+        seen.add((form, dtype))
+    assert len(seen) == len(ALL)
+
+
+@pytest.mark.parametrize("over", [dict(rows=0), dict(cols=0), dict(group=48), dict(N=0), dict(dtype=2), dict(num_cu=-1)])
+def test_plan_refusals(over):
+    a = dict(rows=4, cols=64, group=32, N=1, dtype=0, num_cu=256)
+    out = np.zeros(4, np.int32)
+    assert B.lib.approx_lstm_q4_plan(*a.values(), out.ctypes.data) == 0
+    assert B.lib.approx_lstm_q4_plan(*dict(a, **over).values(), out.ctypes.data) == 1
+    assert B.lib.approx_lstm_q4_plan(*a.values(), None) == 1
+    assert B.lib.approx_lstm_q4_plan(*dict(a, rows=(1 << 25) + 1).values(), out.ctypes.data) == 6
+
+
+def cut(x, bits):
+    """fp32 x without its last mantissa bits, as a kernel that lost a part would see it."""
+    return (x.astype(np.float32).view(np.uint32) & np.uint32(0xFFFFFFFF << (24 - bits) & 0xFFFFFFFF)).view(np.float32).astype(float)
+
+
+@pytest.mark.parametrize("D,G", [(64, 32), (512, 64), (2177, 128)])
+def test_measures_see_a_lost_part_of_x(D, G):
+    q, s, z = levels(200, D, G)
+    x = np.random.default_rng(D).normal(size=(20, D)).astype(np.float32).astype(float)
+    plain = gated.q4_product(q, s, z, G, x)[0].astype(np.float32).astype(float)
+    assert rms_share(plain, q, s, z, G, x) < 0.1
+    for bits in (8, 16):
+        assert rms_share(gated.q4_product(q, s, z, G, cut(x, bits))[0], q, s, z, G, x) > 2.0
+    x, at, v = one_column(20, 200, D, 1)
+    assert one_column_share(gated.q4_product(q, s, z, G, x)[0], q, s, z, G, at, v) < 1e-6
+    for bits in (8, 16):
+        assert one_column_share(gated.q4_product(q, s, z, G, cut(x, bits))[0], q, s, z, G, at, v) > 4.0
