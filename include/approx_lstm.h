@@ -580,7 +580,8 @@ approx_lstm_status approx_lstm_linear_workspace(int32_t T, int32_t B, int32_t H,
  * approx_lstm_q4_run -- y = the product with x device [N][cols] plus bias (device
  * fp32 [rows], or NULL), y device [N][rows].  x and y hold `dtype` (0 = fp32, 1 =
  * bf16), sums are fp32; the levels enter exactly and scales as fp32, so nothing is
- * rounded but the sums and, for bf16, y.  N >= 0 (0: nothing is done).  A row of x
+ * rounded but the sums and, for bf16, y.  N >= 0 (0: nothing is done).  Finite x and
+ * scales of any size give a finite y wherever its type holds the result.  A row of x
  * that holds an infinity or a NaN leaves infinities or NaN in its row of y, in no
  * other.
  * Asynchronous on hip_stream, allocates nothing, can be captured; a matrix is

@@ -41,6 +41,13 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f3
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// the lane's number, of no register that lives until then
+__device__ __forceinline__ int lane_now() {
+  unsigned all = ~0u;
+  asm volatile("" : "+s"(all));
+  return __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+}
+
 // word of the store that holds level (r, d), and its bit
 struct Place {
   size_t word;
@@ -231,6 +238,11 @@ __device__ __forceinline__ float sum8(const f32x8& v) {
 }
 __device__ __forceinline__ float sum8(const bf16x8& v) { return sum8(__builtin_convertvector(v, f32x8)); }
 
+__device__ __forceinline__ bool finite(const f32x4& v) {
+  const float t = __builtin_fmaf(v[3], 0.f, __builtin_fmaf(v[2], 0.f, __builtin_fmaf(v[1], 0.f, v[0] * 0.f)));
+  return t == 0.f;   // (NaN where one is not)
+}
+
 // scales and moved zero levels of four rows
 struct Scale {
   f32x4 s, z;
@@ -261,6 +273,61 @@ __device__ __forceinline__ void store_y(T* y, const float* bias, int R, size_t n
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (r + i < R) p[i] = (T)(v[i] + (bias ? bias[r + i] : 0.f));
+  }
+}
+
+// One result once more, column after column by the formula, in fp64, whose range no sum of
+// products of three fp32 numbers leaves; it stays as it was where that is not finite either
+// (a scale or the bias is not, or y is beyond its type).
+template <class T, int G>
+__device__ __forceinline__ void mend_one(const Q4Matrix& m, const T* row, const float* bias, T* to, int r) {
+  double t = bias ? (double)bias[r] : 0.0;
+#pragma unroll 1
+  for (int d = 0; d < m.D; d += 8) {
+    const size_t at = ((size_t)(r >> 4) * m.padded + d / G) * 16 + (r & 15);
+    const double s = m.s[at];
+    const int z = m.z[at];
+    const unsigned w = m.q[place_of(m, r, d).word];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double v = d + e < m.D ? (double)(float)row[d + e] : 0.0;
+      t = __builtin_fma(s * (double)((int)((w >> (4 * (e / 2 + 4 * (e & 1)))) & 15u) - z), v, t);
+    }
+  }
+  if (fabs(t) < __builtin_inf()) *to = (T)(float)t;
+}
+
+// A finite x from 2^115, or a large scale, takes sums past fp32 where y itself is not:
+// lanes whose sums for row n were not finite (`bad`) do those results (rows r .. r + count
+// - 1 of each of `tiles` row tiles) over, unless the row of x is not finite itself: its
+// results stay as they are.  All lanes of a wave come here, and look through one row of x
+// together at a time (4096 rows with an infinity in each, 2048 x 2048, bf16: 151 us, without
+// 52).  No call with ordinary values gets here.
+template <class T, int G>
+__device__ __forceinline__ void mend(const Q4Matrix& m, const T* x, int n, const float* bias, T* y, int r, int tiles, int count,
+                                     bool bad) {
+  unsigned long long todo = __ballot(bad);
+#pragma unroll 1
+  while (todo) {
+    const int now = __builtin_amdgcn_readlane(n, __builtin_ctzll(todo));
+    const bool mine = bad && n == now;
+    todo &= ~__ballot(mine);
+    const T* row = x + (size_t)now * m.D;
+    bool whole = true;
+#pragma unroll 1
+    for (int k = 8 * lane_now(); k < m.D; k += 512) {
+      const f32x8 v = __builtin_convertvector(load_x<T>(row, k, m.D, false, false), f32x8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) whole = whole && fabsf(v[e]) < __builtin_inff();
+    }
+    if (__all(whole) && mine) {
+#pragma unroll 1
+      for (int i = 0; i < tiles * count; ++i) {
+        const int at = r + 16 * (i / count) + i % count;
+        T* to = y + (size_t)now * m.R + at;
+        if (at < m.R && !(fabsf((float)*to) < __builtin_inff())) mend_one<T, G>(m, row, bias, to, at);
+      }
+    }
   }
 }
 
@@ -356,7 +423,9 @@ __global__ void __launch_bounds__(64 * KW) q4_rows_kernel(Q4Matrix m, const T* x
     f32x4 v = part[0][j][lane];
 #pragma unroll
     for (int k = 1; k < KW; ++k) v += part[k][j][lane];
-    if (n < N && at < m.R) store_y<T>(y, bias, m.R, n, at, v);
+    const bool here = n < N && at < m.R;
+    if (here) store_y<T>(y, bias, m.R, n, at, v);
+    if (__any(here && !finite(v))) mend<T, G>(m, x, n, bias, y, at, 1, 4, here && !finite(v));
   }
 }
 
@@ -437,15 +506,17 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
 #pragma unroll
     for (int n = 0; n < NX; ++n) part[wave][r * NX + n][lane] = acc[r][n];
   __syncthreads();
-  for (int j = threadIdx.x; j < 16 * RT * NX; j += 64 * KW) {
-    const int i = j & 15, r = (j >> 4) / NX, n = (j >> 4) % NX, at = (tile0 + r) * 16 + i;
-    if (n >= N || at >= m.R) continue;
+  for (int j0 = 64 * wave; j0 < 16 * RT * NX; j0 += 64 * KW) {
+    const int j = j0 + lane, i = j & 15, k = min(j >> 4, RT * NX - 1), n = k % NX, at = (tile0 + k / NX) * 16 + i;
+    const bool here = j < 16 * RT * NX && n < N && at < m.R;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < KW; ++k)
+    for (int w = 0; w < KW; ++w)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) v += part[k][j >> 4][16 * g + i];
-    y[(size_t)n * m.R + at] = (T)(v + (bias ? bias[at] : 0.f));
+      for (int g = 0; g < 4; ++g) v += part[w][k][16 * g + i];
+    if (here) y[(size_t)n * m.R + at] = (T)(v + (bias ? bias[at] : 0.f));
+    const bool bad = here && !(fabsf(v) < __builtin_inff());
+    if (__any(bad)) mend<T, G>(m, x, n, bias, y, at, 1, 1, bad);
   }
 }
 
@@ -592,12 +663,21 @@ __global__ void __launch_bounds__(kTileThreads * KS, NT == 4 || KS == 2 || sizeo
 #pragma unroll
     for (int j = 0; j < RT * NT; ++j) acc[j / NT][j % NT] += sums[wave][j][lane];
   }
+  const int now = lane_now(), ci = now & 15, cg = now >> 4;
+  unsigned bad = 0;   // bit t: sums of the t-th 16 rows of x that are not finite
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int n = n0 + 16 * t + li, at = (tile0 + r) * 16 + 4 * lg;
+      const int n = n0 + 16 * t + ci, at = (tile0 + r) * 16 + 4 * cg;
       if (n < N && at < m.R) store_y<T>(y, bias, m.R, n, at, acc[r][t]);
+      bad |= finite(acc[r][t]) ? 0u : 1u << t;
+    }
+  if (__any(bad != 0))
+#pragma unroll 1
+    for (int t = 0; t < NT; ++t) {
+      const int n = n0 + 16 * t + ci;
+      mend<T, G>(m, x, n, bias, y, tile0 * 16 + 4 * cg, RT, 4, n < N && (bad >> t & 1));
     }
 }
 

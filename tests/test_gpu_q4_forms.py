@@ -55,3 +55,50 @@ def test_every_kernel(form, dtype, G):
             d = torch.from_numpy((q[:, at].astype(np.int64) - z[:, at // G]).T * s[:, at // G].T.astype(np.float64)).cuda()
             want = d * x.double()[torch.arange(N, device="cuda"), torch.from_numpy(at).cuda()][:, None]
             assert torch.equal(got, want.to(BF16))
+
+
+@pytest.mark.parametrize("form,dtype", ALL, ids=IDS)
+def test_the_largest_values_of_x(form, dtype):
+    """Finite rows of x up to the type's largest number have finite rows of y
+    wherever that is what the product is, infinities of its sign where it is
+    beyond, and change no bit of another row; infinities and NaN stay."""
+    N, R, widths = FORMS[form]
+    D, G, big = widths[-1], 64, float(torch.finfo(dtype).max)
+    say(form, dtype, D)
+    q, s, z = levels(R, D, G)
+    s = (s * 2.0 ** -12).astype(np.float32)
+    s[::3] *= 4096   # the largest number times these and more than one level is beyond fp32
+    m, r = load(q, s, z, G), np.random.default_rng([2, N, D])
+    x = place(r.normal(size=(N, D)), dtype)
+    clean = product(m, x, dtype)
+    rows = sorted({0, N // 2, N - 1})
+    at = r.integers(0, D, len(rows))
+    for n, d in zip(rows, at):
+        x[n] = 0
+        x[n, d] = big if n else -big
+    y = product(m, x, dtype)
+    keep = [n for n in range(N) if n not in rows]
+    assert torch.equal(y[keep], clean[keep])
+    v = x.double()[rows, torch.from_numpy(at).cuda()].cpu().numpy()
+    d = (q[:, at].astype(np.float64) - z[:, at // G]).T
+    sd = s[:, at // G].T.astype(np.float64)
+    want = torch.from_numpy(d * sd * v[:, None]).float().double().numpy()
+    got = y[rows].double().cpu().numpy()
+    near = np.abs(want) < 0.99 * big
+    # roundings as in one_column_share (bf16: exact but for the scale), then the output's
+    tol = 2.0 ** -24 * sd * np.abs(v)[:, None] * (2.1 * 15 + 15 + 2 * np.abs(d)) + {F32: 2.0 ** -24, BF16: 2.0 ** -8}[dtype] * np.abs(want)
+    assert near.any() and (np.abs(got[near] - want[near]) <= 1.01 * tol[near]).all()
+    far = np.isinf(want)
+    assert far.any() and (got[far] == want[far]).all()
+    # two that cancel, in one group: what is left is theirs times the difference of their levels
+    if D > 1:
+        x[rows[0]] = 0
+        x[rows[0], 0], x[rows[0], 1] = big, -big
+        got = product(m, x, dtype)[rows[0]].double().cpu().numpy()
+        want = (q[:, 0].astype(np.float64) - q[:, 1]) * s[:, 0] * big
+        near = np.abs(want) < 0.99 * big
+        tol = 2.0 ** -24 * s[:, 0].astype(np.float64) * big * (6 * 15 + 4 * 15) + {F32: 2.0 ** -24, BF16: 2.0 ** -8}[dtype] * np.abs(want)
+        assert near.any() and (np.abs(got[near] - want[near]) <= 1.01 * tol[near]).all()
+    for bad in (float("inf"), float("nan")):
+        x[rows[0], D - 1] = bad
+        assert not torch.isfinite(product(m, x, dtype)[rows[0]]).any()
