@@ -728,14 +728,16 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 // What both sides took, in us, D = 2048 unless given:
-// - many rows of x: the tile kernel once half the compute units get a workgroup of it;
-//   64 rows of x at a time where that makes two a unit (bf16, 4096 x 2048: 49, 32 at a
+// - many rows of x: the tile kernel once the row kernel (32 of them and 64 of the matrix a
+//   workgroup) makes more than two workgroups a unit.  Row kernel / tile kernel: two a
+//   unit, R = 2048, N = 512, bf16 16.8 / 18.7, fp32 28.7 / 31.6, R = 8192, N = 128 16.3 / 19.9,
+//   28.9 / 33.9 (but N > R, x past the caches: R = 256, N = 4096 18.8 / 18.0, 40 / 32.5); more,
+//   N = 640 23.4 / 18.7, 41 / 32; N = 1024 31 / 19, 54 / 33; R = 256, N = 8192 34 / 20, 69 /
+//   37.  64 rows of x at a time where that makes two a unit (bf16, 4096 x 2048: 49, 32 at a
 //   time 54; 2048 x 2048: 36 and 31), in fp32 always 32 (8192 x 2048: 211, 64 at a time
 //   254 with spilled registers); the columns in two halves where there is at most a
 //   workgroup a unit (R = 2048, N = 1024, bf16 19, whole 23, fp32 34 and 40; R = 3716, D =
-//   2951, N = 730, 345 workgroups: 52 and 45).  Row kernel / tile kernel: R = 2048, N =
-//   256, bf16 9 / 18, fp32 15 / 31; N = 512 16.5 / 18.7, 46 / 31; N = 1024 42 / 19, 89 / 34;
-//   R = 256, D = 4096, N = 4096 50 / 36, 76 / 63.
+//   2951, N = 730, 345 workgroups: 52 and 45).
 // - one row, in fp32 two: the dot kernel (fp32, G = 32, R = 32768, D = 8192: 40, row
 //   kernel 113; R = 2048, D = 8256: 10, 16), as many row tiles a workgroup as leave
 //   two workgroups a unit, and sixteen waves where there are fewer than one (R = 2048,
@@ -751,7 +753,7 @@ Q4Form q4_form(const Q4Matrix& m, int N, int bf16, int num_cu) {
   const size_t wide = cover(m.R, kTileRows) * cover(N, 64), narrow = cover(m.R, kTileRows) * cover(N, 32);
   if (N > 64 && bf16 && wide >= 2 * cu) return {kQ4Tile, 4, 4, 1};
   if (N > 64 && narrow > cu) return {kQ4Tile, 4, 2, 1};
-  if (N > 64 && 2 * narrow >= cu) return {kQ4Tile, 4, 2, 2};
+  if (N > 64 && (2 * narrow > cu || (2 * narrow == cu && N > m.R))) return {kQ4Tile, 4, 2, 2};
   if (N == 1 && tiles >= 4 * cu) return {kQ4Dot, 4, 1, 8};
   if (N == 1 && tiles >= 2 * cu) return {kQ4Dot, 2, 1, 8};
   if (N == 1) return {kQ4Dot, 1, 1, 16};

@@ -57,3 +57,13 @@ def test_measures_see_a_lost_part_of_x(D, G):
     assert one_column_share(gated.q4_product(q, s, z, G, x)[0], q, s, z, G, at, v) < 1e-6
     for bits in (8, 16):
         assert one_column_share(gated.q4_product(q, s, z, G, cut(x, bits))[0], q, s, z, G, at, v) > 4.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_two_row_workgroups_a_unit_stay_with_the_row_kernel(dtype):
+    """Where the row kernel fills the device exactly twice it is the faster one;
+    from there on, and where x is larger than the matrix, the tile kernel is."""
+    for R, N in ((2048, 512), (8192, 128), (4096, 256)):
+        assert B.approx_lstm_q4_plan(R, 2048, 128, N, dtype, 256) == ("rows", 4, 2, 8)
+        assert B.approx_lstm_q4_plan(R, 2048, 128, N + 32, dtype, 256) == ("tile", 4, 2, 2)
+    assert B.approx_lstm_q4_plan(256, 2048, 128, 4096, dtype, 256) == ("tile", 4, 2, 2)
