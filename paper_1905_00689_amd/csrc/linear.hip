@@ -177,7 +177,7 @@ __device__ __forceinline__ float gate_tanh(float y) {
   return fabsf(y) < 0.4f ? near : far;
 }
 
-// Few timesteps: a lane walks its two units through all of them, the loads of
+// Few timesteps (walked): a lane walks its two units through all of them, the loads of
 // kAhead timesteps at once (one token of 32 sequences, H = 1024: 3.2 us; 256 sequences of
 // 16, H = 512: 8.3 us, 21 MB).
 template <class T, Rows R>
@@ -601,9 +601,20 @@ struct Plan {
   int rows;              // of dpart
 };
 
-// columns of 64 pairs of units; chunks of time of one; both together (few: up to 16
-// timesteps, of which a backward pass makes one short chunk)
-constexpr int kFew = 16;
+// Up to how many timesteps the walk is the faster forward kernel: the scan splits 9
+// timesteps and more over waves, but those are there anyway once there are many
+// columns.  Walk / scan in us, bf16: 1 sequence of 512 units, T = 8 6.7 / 6.5, 16 7.1 / 6.5; 32
+// of 1024 (a column a compute unit), T = 8 6.8 / 6.6, 16 8.0 / 6.7, 24 10.0 / 6.6; 64 (two), T =
+// 16 7.9 / 7.5; 96 (three), T = 8 7.5 / 7.6, 16 9.0 / 9.1 (fp32 9.5 / 12.5), 24 11.6 / 10.6; 128
+// (four), T = 16 9.2 / 11.3, 24 11.9 / 12.5, 32 14.6 / 13.9; 512 of 512 units, T = 8 8.3 / 17.2, 24
+// 17.5 / 23.9, 32 22.5 / 26.6.
+int walked(size_t cols, int num_cu) { return cols >= 4 * (size_t)num_cu ? 24 : cols > 2 * (size_t)num_cu ? 16 : 8; }
+
+// columns of 64 pairs of units; chunks of time of one; both together.  A backward pass of
+// two waves' timesteps makes one chunk of two waves (a workgroup of eight would hold waves
+// of padding: 256 sequences of 512 units, forward and back, bf16, T = 16 24.6 us, with eight
+// 35.6; T = 1 20 and 30).
+constexpr int kFew = 2 * kSteps;
 size_t cols_of(int B, int H) { return ((size_t)B * ((H + 1) / 2) + 63) / 64; }
 int chunks_of(int T, int backward) {
   const int chunk = backward && T <= kFew ? kFew : kChunk;
@@ -620,7 +631,7 @@ Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   p.s.cols = (int)cols_of(B, H);
   p.few = T <= kFew;
   p.s.chunks = chunks_of(T, backward);
-  p.walk = !backward && p.few;
+  p.walk = !backward && T <= walked(p.s.cols, num_cu);
   // Forward, chunks side by side where there are at least four and the columns
   // alone leave compute units with fewer than two workgroups (bf16, H = 512, T = 512,
   // side by side / one after another: 64 sequences 46 / 46 us, 128 89 / 78, 256 162 /
