@@ -511,6 +511,7 @@ void approx_lstm_exact_destroy(approx_lstm_exact* m);
  *            NULL where that is 0.  Its contents need not be kept or cleared;
  *            calls that may overlap (two streams, two captured graphs replayed
  *            at once) need one each
+ * An infinite c0 comes out infinite or NaN (time is summed in pieces).
  * T = 0 copies c0 to c_out.  Asynchronous on hip_stream, allocates nothing, can
  * be captured.  p, h_out and c_save must not overlap.
  *

@@ -446,6 +446,9 @@ def _on(t, name, shape, dtype, index):
 def _launch(index, stream, call):
     """call(stream handle) with GPU `index` current; its status checked.  stream:
     None (the current one of that GPU), a torch stream or a handle."""
+    of = getattr(stream, "device_index", index)   # (kernels run where their stream is)
+    if of != index:
+        raise ValueError(f"stream is of GPU {of}, not of {index}")
     before = torch.cuda.current_device()
     if before == index:
         status = call(_raw_stream(index) if stream is None else _stream(stream))
@@ -569,8 +572,9 @@ def approx_lstm_q4_prepare(w, group=128, stream=None):
         raise ValueError(f"w has shape {w.shape}, expected (rows, cols)")
     out = ctypes.c_void_p()
     rows, cols, group = _int32(w.shape[0], "rows"), _int32(w.shape[1], "cols"), _int32(int(group), "group")
-    _check(lib.approx_lstm_q4_prepare(wp, rows, cols, group, _stream(stream), ctypes.byref(out)))
-    return Q4Matrix(out.value, rows, cols, group, torch.cuda.current_device())
+    index = torch.cuda.current_device()
+    _launch(index, stream, lambda s: lib.approx_lstm_q4_prepare(wp, rows, cols, group, s, ctypes.byref(out)))
+    return Q4Matrix(out.value, rows, cols, group, index)
 
 
 def approx_lstm_q4_load(q, scale, zero, cols, group=128, stream=None):

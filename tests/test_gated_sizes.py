@@ -59,3 +59,18 @@ def test_tensors_of_more_than_2_32_rows_are_refused():
     m = B.approx_lstm_q4_prepare(np.ones((1, 1), np.float32), 32)
     with pytest.raises(ValueError):
         B.approx_lstm_q4_run(m, h.view(n + 5, 1), torch.empty_like(h).view(n + 5, 1))
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    """A kernel runs on its stream's GPU, where the tensors are not."""
+
+    class Stream:
+        device_index, cuda_stream = 1, 4096
+
+    called = []
+    monkeypatch.setattr(B, "_linear_workspace", lambda *a: 64)
+    with pytest.raises(ValueError, match="GPU 1"):
+        B._launch(0, Stream(), called.append)
+    with pytest.raises(ValueError, match="GPU 1"):
+        B._linear_call(lambda *a: called.append(a), 5, 1, 64, 0, 0, None, Stream(), ())
+    assert not called
