@@ -184,8 +184,10 @@ __device__ __forceinline__ typename XVec<T>::Raw load_x(const T* row, int k, int
     v = load_eight<T>(row + k, odd);
   } else if (k < D) {   // (eight loads at once, not one after another)
     T t[8];
+    int last = D - 1;
+    asm volatile("" : "+s"(last));   // (the row's end found here: kept from before a loop it would take registers there)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = row[min(k + e, D - 1)];
+    for (int e = 0; e < 8; ++e) t[e] = row[min(k + e, last)];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = k + e < D ? t[e] : (T)0.f;
   }
