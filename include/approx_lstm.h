@@ -490,8 +490,8 @@ void approx_lstm_exact_destroy(approx_lstm_exact* m);
  *
  * Stateless calls on the current device.  p, h_out and their gradients hold
  * `dtype` (0 = fp32, 1 = bf16); the state, the bias and their gradients are
- * fp32, and so is all arithmetic.  Results do not depend on the device's load:
- * every sum has a fixed order.
+ * fp32, and so is all arithmetic (tanh within 5e-7 of itself, however small).  Results
+ * do not depend on the device's load: every sum has a fixed order.
  *
  * approx_lstm_linear_run -- the recurrence over a sequence, or (T = 1) one token.
  *   p        device [T][B][4H]

@@ -11,18 +11,19 @@
 // its 8 steps from its own first state, so p is read once and nothing but maps is
 // exchanged.  Every composition has a fixed order: same bits whatever runs beside.
 //
-// What bounds it is memory, with the vector units close behind in bf16 (48 instructions
-// an element, ten of them transcendental).  MI355X, where a large copy moves 5.2 TB/s:
-// bf16, T = 4096, H = 8192, 335 MB in 82 us (4.1 TB/s); T = 65536, H = 512, the same bytes
-// in 97 us, 14 of them for the longer chain of states; 256 sequences of 512, H = 512,
-// 155 us (4.3 TB/s).  Forward and back, 8 x 2048, H = 1024: 127 us, of which 38 the
-// forward kernel, 70 the backward one (310 MB, 4.4 TB/s), 5 the bias gradient's sums and
-// 10 the clearing of the words that chunks hand over with.
+// What bounds it is memory and the vector units together (64 instructions an element
+// forward, ten of them transcendental and fourteen for tanh near 0; in bf16 busy 72% of the
+// time).  MI355X, where a large copy moves 5.2 TB/s: bf16, T = 4096, H = 8192, 335 MB in 90
+// us (3.7 TB/s); T = 65536, H = 512, the same bytes in 101 us, 11 of them for the longer
+// chain of states; 256 sequences of 512, H = 512, 156 us (4.3 TB/s).  Forward and back,
+// 8 x 2048, H = 1024: 135 us, 50 forward and 86 back by themselves, of which 5 each clear the
+// words that chunks hand over with and 7 sum the bias gradient (the backward kernel 310 MB
+// in 73, 4.2 TB/s).
 //
 // Tried and dropped: a flag for each map instead of maps that carry their own sign
 // (less to clear, but the wait for the stores' acknowledgement costs 15 us at every
 // size); maps cleared by nontemporal stores (+2 us); registers cut to 64 by spilling
-// (82 -> 96 us).
+// (+14 us at T = 4096, H = 8192).
 #include <algorithm>
 #include <type_traits>
 
@@ -178,8 +179,8 @@ __device__ __forceinline__ float gate_tanh(float y) {
 }
 
 // Few timesteps (walked): a lane walks its two units through all of them, the loads of
-// kAhead timesteps at once (one token of 32 sequences, H = 1024: 3.2 us; 256 sequences of
-// 16, H = 512: 8.3 us, 21 MB).
+// kAhead timesteps at once (one token of 32 sequences, H = 1024: 3.3 us; 256 sequences of
+// 16, H = 512: 9.1 us, 21 MB).
 template <class T, Rows R>
 __global__ void __launch_bounds__(kWalkThreads) linear_walk_kernel(LinearArgs a) {
   constexpr int kAhead = 4;
@@ -239,7 +240,7 @@ constexpr f32x4 kIdentity{1.f, 0.f, 1.f, 0.f};
 // state that the group before handed on: a hop of the serial chain passes a whole
 // group, and a chunk reads 7 maps on average.  (One level of 32 chunks, 16 maps on
 // average, took 121 us instead of 113 at T = 65536, H = 512, bf16; then one lane that
-// looks for a wave instead of all 64 brought it to 96.)
+// looks for a wave instead of all 64 brought it to 96; tanh near 0 then cost 5.)
 //
 // Which chunk a workgroup takes is the ticket of its column: in the order in which
 // workgroups start, so the chunks that anyone waits for have workgroups that run.
@@ -634,10 +635,11 @@ Plan plan_of(int T, int B, int H, int num_cu, int backward) {
   p.walk = !backward && T <= walked(p.s.cols, num_cu);
   // Forward, chunks side by side where there are at least four and the columns
   // alone leave compute units with fewer than two workgroups (bf16, H = 512, T = 512,
-  // side by side / one after another: 64 sequences 46 / 46 us, 128 89 / 78, 256 162 /
-  // 155; T = 100, H = 64, two chunks: 17 / 9.6 us, the words' clearing is a launch).
-  // Backward always: the loop needs more registers than there are (the same shapes
-  // forward and back: 126 / 126, 249 / 259, 460 / 510 us).  A grid has fewer than 2^32
+  // side by side / one after another: 64 sequences 49 / 48 us, 96 68 / 74, 128 93 / 82, 256
+  // 173 / 159; H = 64, T = 100, two chunks, 12.7 / 10.6, T = 200, four, 12.2 / 17.3: the words'
+  // clearing is a launch).  Backward always: a loop needs more registers than there are
+  // (as long as there was one, 64, 128 and 256 sequences forward and back took 126 / 126,
+  // 249 / 259, 460 / 510 us).  A grid has fewer than 2^32
   // threads: beyond, forward takes the loop and backward is refused.
   const size_t pieces = pieces_of(T, B, H, backward);
   p.look = !p.walk && p.s.chunks > 1 &&

@@ -285,7 +285,7 @@ template <class T, int G>
 __device__ __forceinline__ void mend_one(const Q4Matrix& m, const T* row, const float* bias, T* to, int r) {
   double t = bias ? (double)bias[r] : 0.0;
 #pragma unroll 1
-  for (int d = 0; d < m.D; d += 8) {
+  for (int d = 0; d < m.D && fabs(t) < __builtin_inf(); d += 8) {
     const size_t at = ((size_t)(r >> 4) * m.padded + d / G) * 16 + (r & 15);
     const double s = m.s[at];
     const int z = m.z[at];
@@ -336,8 +336,8 @@ __device__ __forceinline__ void mend(const Q4Matrix& m, const T* x, int n, const
 // Few rows of x: what bounds it is reading the matrix, so every workgroup reads RT
 // row tiles of it once, its KW waves every KW-th block of columns, for up to 16 NT
 // rows of x straight from L2; the waves' sums meet in LDS, in order.  A few blocks a wave
-// leave it to latency: 48 rows of x, 8192 x 2048, bf16 10.7 us (10 MB and 0.4 MB of
-// scales); 16 rows, 32768 x 8192 39 us (145 MB, 3.7 TB/s).  fp32 is bound by splitting x
+// leave it to latency: 48 rows of x, 8192 x 2048, bf16 8.7 us (G = 128: 8.4 MB of levels and 0.7
+// of scales; G = 64 11.1); 16 rows, 32768 x 8192 39 us (145 MB, 3.7 TB/s).  fp32 is bound by splitting x
 // (44 operations a step of 32 columns, 22 for the levels): 100 rows of 8256 columns, 256
 // rows of the matrix, G = 32: 22 us on 112 compute units.  Loading x a block ahead too
 // changes nothing.
@@ -528,8 +528,8 @@ __global__ void __launch_bounds__(64 * KW) q4_dot_kernel(Q4Matrix m, const T* x,
 // there a block of columns at a time, the next block's loads under way meanwhile; with
 // KS = 2 there are eight, the second four on every other block of columns.  The
 // group sums of x are formed by the threads that stage it, and the scales stand beside
-// them.  4096 rows of x, 2048 x 2048, bf16, G = 128: 46 us (750 TFLOP/s, a large library
-// product in bf16 1210); R = 8192 169 us (815).  A wave's block is 64 matrix
+// them.  4096 rows of x, 2048 x 2048, bf16, G = 128: 45 to 50 us (690 to 764 TFLOP/s, a large
+// library product in bf16 1210 to 1280); R = 8192 181 us (760).  A wave's block is 64 matrix
 // instructions (1024 cycles) and 380 others (1500): bound by those and, at two
 // waves a unit, by the wait for the next block of x.  Tried: loads two blocks ahead in
 // registers (spills: 57 us); scales read at the end of a group instead of staged (67).
