@@ -623,6 +623,7 @@ def approx_lstm_q4_plan(rows, cols, group, N, dtype=torch.float32, num_cu=0):
     """The kernel that a product with N rows of x takes (no device work where num_cu is
     given): ("dot", "rows" or "tile", its row tiles, its rows of x, its split)."""
     out = np.zeros(4, np.int32)
-    sizes = [_int32(int(v), name) for v, name in ((rows, "rows"), (cols, "cols"), (group, "group"), (N, "N"))]
-    _check(lib.approx_lstm_q4_plan(*sizes, _DTYPES[dtype], int(num_cu), out.ctypes.data))
+    rows, cols, group, N, num_cu = (_int32(int(v), name) for v, name in (
+        (rows, "rows"), (cols, "cols"), (group, "group"), (N, "N"), (num_cu, "num_cu")))
+    _check(lib.approx_lstm_q4_plan(rows, cols, group, N, _DTYPES[dtype], num_cu, out.ctypes.data))
     return (("dot", "rows", "tile")[out[0]], *(int(v) for v in out[1:]))
